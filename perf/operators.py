@@ -1,11 +1,11 @@
 """The operators of the 8-bit feed-forward block, dense and by experts, as cases to measure.
 
 One pass is one call of one of the single operations that ``metro_ops.h``
-declares for it: the RMSNorm that adds a projection's result to the residual and
-writes 8-bit rows, the block-scaled product of 8-bit rows and weights (with the
-residual's addition or SwiGLU behind it), the router of tokens to experts, the
-same product with each expert's rows, and the weighted sum that brings the
-experts' rows back to their tokens.  The widths are those of ``synth``
+declares for it: the RMSNorm that adds a projection's bf16 rows to the residual
+and writes 8-bit rows, the block-scaled product of 8-bit rows and weights (to
+bf16 rows, or with SwiGLU behind it to 8-bit rows), the router of tokens to
+experts, the same product with each expert's rows, and the weighted sum that
+adds the experts' rows to their tokens' residual.  The widths are those of ``synth``
 (Llama-3-8B and 70B layers, the tiny test model), the row counts those of the
 agents' calls.
 
@@ -37,8 +37,8 @@ def listed():
         dict(name="gate_up_25", kind="gemm", M=25, N=28672, K=4096, epilogue=2),
         # A large ready batch, an odd number of rows, through the attention's projections.
         dict(name="qkv_301", kind="gemm", M=301, N=6144, K=4096, epilogue=0),
-        # A 70B layer's way back to the residual at its benchmark batch.
-        dict(name="down_70b_128", kind="gemm", M=128, N=8192, K=28672, epilogue=1),
+        # A 70B layer's feed-forward back to the model's width at its benchmark batch.
+        dict(name="down_70b_128", kind="gemm", M=128, N=8192, K=28672, epilogue=0),
         # A prefill forward of sixteen 512-token chunks.
         dict(name="gate_up_8192", kind="gemm", M=8192, N=28672, K=4096, epilogue=2),
         # The router of a decode batch: softmax over eight experts, two for each token.
@@ -60,8 +60,8 @@ def _log_int(rng, lo, hi):
 
 
 # (N, K, epilogue) of a layer's products: 8B QKV, gate/up, down; 70B gate/up, down; tiny gate/up, down; odd ones
-_PRODUCTS = [(6144, 4096, 0), (28672, 4096, 2), (4096, 14336, 1), (57344, 8192, 2), (8192, 28672, 1), (1376, 256, 2),
-             (256, 768, 1), (1056, 640, 0), (2080, 1408, 2), (4000, 896, 1)]
+_PRODUCTS = [(6144, 4096, 0), (28672, 4096, 2), (4096, 14336, 0), (57344, 8192, 2), (8192, 28672, 0), (1376, 256, 2),
+             (256, 768, 0), (1056, 640, 0), (2080, 1408, 2), (4000, 896, 0)]
 
 
 def draw(rng):
@@ -106,13 +106,13 @@ def work(case):
     kind = case["kind"]
     if kind == "norm":
         n, g = case["rows"] * case["d"], case["rows"] * (_pad(case["d"]) // GROUP)
-        return {"bytes": n * (4 + 1 + (8 if case["delta"] else 0) + (2 if case["bf16"] else 0)) + g + 2 * case["d"], "flops": 6 * n}
+        return {"bytes": n * (4 + 1 + (6 if case["delta"] else 0) + (2 if case["bf16"] else 0)) + g + 2 * case["d"], "flops": 6 * n}
     if kind == "route":
         T, E, k = case["T"], case["E"], case["k"]
         return {"bytes": 4 * T * E + 4 * T * k * 4 + 4 * (E + 1), "flops": T * E * (8 + k)}
     if kind == "combine":
         n = case["T"] * case["d"]
-        return {"bytes": 4 * n * (case["k"] + 2) + 8 * case["T"] * case["k"], "flops": 2 * n * case["k"]}
+        return {"bytes": n * (2 * case["k"] + 8) + 8 * case["T"] * case["k"], "flops": 2 * n * case["k"]}
     N, K = case["N"], case["K"]
     weight = N * K + N * (K // GROUP)
     if kind == "gemm":
@@ -120,7 +120,7 @@ def work(case):
     else:
         chosen = _assigned(case["T"], case["E"], case["k"])
         M, rows, weights = chosen.size, case["T"] if case["epilogue"] == 2 else chosen.size, len(np.unique(chosen))
-    out = {0: 4 * M * N, 1: 8 * M * N, 2: M * (N // 2 + N // 2 // GROUP)}[case["epilogue"]]
+    out = M * (N // 2 + N // 2 // GROUP) if case["epilogue"] == 2 else 2 * M * N
     return {"bytes": weights * weight + rows * (K + K // GROUP) + out, "flops": 2 * M * N * K}
 
 
@@ -184,7 +184,7 @@ def prepare(case, seed):
     if kind == "norm":
         rows, d = case["rows"], case["d"]
         x = _normal(g, rows, d) * torch.exp2(torch.randint(-2, 3, (rows, 1), generator=g, device=DEV).float())
-        return dict(kind=kind, x=x, delta=0.5 * _normal(g, rows, d) if case["delta"] else None,
+        return dict(kind=kind, x=x, delta=(0.5 * _normal(g, rows, d)).to(torch.bfloat16) if case["delta"] else None,
                     gain=(1.0 + 0.1 * _normal(g, d)).to(torch.bfloat16), rows=rows, d=d,
                     x_out=torch.empty_like(x) if case["delta"] else None,
                     h16=torch.empty(rows, d, dtype=torch.bfloat16, device=DEV) if case["bf16"] else None,
@@ -198,18 +198,18 @@ def prepare(case, seed):
                     offsets=torch.empty(E + 1, dtype=torch.int32, device=DEV),
                     src=torch.empty(T * k, dtype=torch.int32, device=DEV),
                     slot=torch.empty(T, k, dtype=torch.int32, device=DEV),
-                    ws=torch.empty(-(-T // 256) * E, dtype=torch.int32, device=DEV))
+                    ws=torch.empty(-(-T // 64) * E, dtype=torch.int32, device=DEV))
     if kind == "combine":
         T, k, d = case["T"], case["k"], case["d"]
         w = torch.rand(T, k, generator=g, device=DEV) + 0.1
-        return dict(kind=kind, y=_normal(g, T * k, d), x=_normal(g, T, d), weights=w / w.sum(1, keepdim=True), T=T, k=k, d=d,
+        return dict(kind=kind, y=_normal(g, T * k, d).to(torch.bfloat16), x=_normal(g, T, d), weights=w / w.sum(1, keepdim=True), T=T, k=k, d=d,
                     slot=torch.randperm(T * k, generator=g, device=DEV).to(torch.int32).reshape(T, k),
                     out=torch.empty(T, d, device=DEV))
     N, K, epi = case["N"], case["K"], case["epilogue"]
     if kind == "gemm":
         T = M = case["M"]
         weights = [_quantise(0.02 * _normal(g, N, K))]
-        s = dict(kind=kind, resid=_normal(g, M, N) if epi == 1 else None)
+        s = dict(kind=kind)
     else:
         T, E, k = case["T"], case["E"], case["k"]
         M = T * k
@@ -234,7 +234,7 @@ def prepare(case, seed):
         s.update(out=torch.empty(M, _pad(cols), dtype=torch.uint8, device=DEV),
                  out_scale=torch.full((M, _pad(_pad(cols) // GROUP, 4)), 127, dtype=torch.uint8, device=DEV))
     else:
-        s.update(out=torch.empty(M, N, device=DEV), out_scale=None)
+        s.update(out=torch.empty(M, N, dtype=torch.bfloat16, device=DEV), out_scale=None)
     return s
 
 
@@ -259,7 +259,7 @@ def _run_norm(s):
         metro.op_rmsnorm_fp8(s["x"], s["gain"], EPS, s["h"], s["h_scale"], s["rows"], d, delta=s["delta"], x_out=s["x_out"],
                              h_bf16=s["h16"])
         return {"x": s["x_out"], "h16": s["h16"], **_eight(s["h"], s["h_scale"], d)}
-    x = s["x"] if s["delta"] is None else s["x"] + s["delta"]
+    x = s["x"] if s["delta"] is None else s["x"] + s["delta"].to(torch.float32)
     h = x * torch.rsqrt((x * x).mean(1, keepdim=True) + EPS) * s["gain"].to(torch.float32)
     codes, scale = _quantise(h)
     return {"x": None if s["delta"] is None else x, "h16": None if s["h16"] is None else h.to(torch.bfloat16),
@@ -307,7 +307,7 @@ def _run_combine(s):
         from paper_2411_03519_amd import metro
         metro.op_combine_experts(s["y"], s["T"] * s["k"], s["weights"], s["slot"], s["T"], s["k"], s["d"], s["out"], resid=s["x"])
         return s["out"]
-    return s["x"] + (s["weights"].unsqueeze(2) * s["y"][s["slot"].long()]).sum(1)
+    return s["x"] + (s["weights"].unsqueeze(2) * s["y"][s["slot"].long()].to(torch.float32)).sum(1)
 
 
 def _run_gemm(s):
@@ -315,12 +315,12 @@ def _run_gemm(s):
     if own:
         from paper_2411_03519_amd import metro
         metro.op_gemm_fp8(s["x"], s["x_scale"], s["packed"], s["packed_scale"], s["M"], N, K, epi, s["out"],
-                          out_scale=s["out_scale"], resid=s["resid"], workspace=s["ws"])
+                          out_scale=s["out_scale"], workspace=s["ws"])
         return _eight(s["out"], s["out_scale"], N // 2) if epi == 2 else s["out"]
     y = _values(s["x"], s["x_scale"][:, :K // GROUP]) @ _values(s["w"][0], s["w_scale"][0]).t()
     if epi == 2:
         return _eight(*_quantise(_gated(y)), N // 2)
-    return s["resid"] + y if epi == 1 else y
+    return y.to(torch.bfloat16)
 
 
 def _run_experts(s):
@@ -335,7 +335,7 @@ def _run_experts(s):
         x = x[s["src"].long()]
     o = s["offsets_host"]
     y = torch.cat([x[o[e]:o[e + 1]] @ _values(s["w"][e], s["w_scale"][e]).t() for e in range(s["E"]) if o[e + 1] > o[e]])
-    return _eight(*_quantise(_gated(y)), N // 2) if epi == 2 else y
+    return _eight(*_quantise(_gated(y)), N // 2) if epi == 2 else y.to(torch.bfloat16)
 
 
 _RUN = {"norm": _run_norm, "route": _run_route, "combine": _run_combine, "gemm": _run_gemm, "experts": _run_experts}
@@ -414,8 +414,6 @@ def exact(case, seed):
     x = _exact_values(s["x"], s["x_scale"])
     if kind == "gemm":
         y = torch.matmul(x, _exact_values(s["w"][0], s["w_scale"][0]).t())
-        if case["epilogue"] == 1:
-            y += s["resid"].double()
     else:
         y = torch.zeros(s["M"], case["N"], dtype=torch.float64, device=DEV)
         for e in range(s["E"]):
