@@ -147,6 +147,143 @@ metro_status metro_op_attn_decode_noalloc(const uint16_t* q, const uint16_t* kv,
                                           int32_t nkv, int32_t hd, int32_t rows, const int32_t* ctx,
                                           const int32_t* block_tables, uint16_t* out, void* stream);
 
+/* --- 8-bit feed-forward: rows, weights and products of e4m3 values ----------
+ *
+ * 8-bit rows: row-major e4m3 codes (1 sign, 4 exponent, 3 mantissa bits; largest
+ * finite value 448) [rows, ld], and for each 128 consecutive values of a row one
+ * byte E in [rows, lds]: the values are code * 2^(E - 127).  A group's power of
+ * two is the smallest that brings its largest magnitude within 448 (at least
+ * 2^-126); codes are rounded from fp32 to nearest, ties to even.  An infinite or
+ * NaN value becomes a NaN code; NaNs do not count for the power, an infinity
+ * makes it 2^120.  Values behind the last column of a partly
+ * filled group are zero codes; bytes of a row's stride behind its last group
+ * are left as they were, and no result hangs on what they hold.
+ *
+ * The feed-forward block of a Llama layer in them: metro_op_rmsnorm_fp8 (adds
+ * the attention's output projection to the residual), metro_op_gemm_fp8 with
+ * gate and up (SwiGLU), metro_op_gemm_fp8 with down (bf16 rows, which the next
+ * layer's metro_op_rmsnorm_fp8 adds).  By experts: metro_op_rmsnorm_fp8 (with
+ * h_bf16), metro_op_gemm with the router's weights, metro_op_route,
+ * metro_op_gemm_fp8_experts with gate and up and src, the same with down, and
+ * metro_op_combine_experts.
+ *
+ * All are asynchronous on `stream`, allocate nothing and may be captured into a
+ * graph; a workspace belongs to one call at a time. */
+
+/* Weights of the 8-bit products.  The bf16 matrix W [N, Kp] (as for
+ * metro_op_pack_weight: W[n, k] = W_rowmajor[n * ld + k] for k < K, 0 for K <= k <
+ * Kp) in 8 bits, a power of two for each row's 128 columns, in matrix-core
+ * operand order: code of W[n, k] at byte
+ *   ((n/16 * Kp/128 + k/128) * 2 + (k/64)%2) * 1024 + (n%16 + 16 * ((k/16)%4)) * 16 + k%16
+ * of W_packed (N * Kp bytes) and the byte E of row n, columns 128 b .. 128 b + 127 at
+ *   ((n/16 * G/4 + b/4) * 16 + n%16) * 4 + b%4
+ * of W_scale (N * G bytes), G = Kp / 128 rounded up to a multiple of 4.
+ * W_packed and W_scale 16-byte aligned.  N % 16 == 0, Kp % 128 == 0, 0 < K <= Kp,
+ * ld >= K.  Errors: E_INVAL. */
+metro_status metro_op_pack_weight_fp8(const uint16_t* W_rowmajor, int32_t ld, int32_t N, int32_t K, int32_t Kp,
+                                      uint8_t* W_packed, uint8_t* W_scale, void* stream);
+
+/* Residual addition, RMSNorm and 8-bit rows in one pass over the residual:
+ *   x'[r, :] = x[r, :] + delta[r, :]                  (x where delta is NULL)
+ *   v[r, :]  = x'[r, :] / sqrt(mean(x'[r, :]^2) + eps) * g       (fp32)
+ * h, h_scale <- v as 8-bit rows; h_bf16 <- bf16(v) unless NULL; x_out <- x'
+ * unless NULL (x_out only with delta; it may be x).
+ *   x, x_out  fp32 [rows, ldx], 16-byte aligned, ldx % 4 == 0
+ *   delta     bf16 [rows, ldd] or NULL, 8-byte aligned, ldd % 4 == 0
+ *   g         bf16 [d], 8-byte aligned
+ *   h_bf16    bf16 [rows, ldh_bf16] or NULL, 8-byte aligned, ldh_bf16 % 4 == 0
+ *   h         e4m3 [rows, ldh], 4-byte aligned, ldh % 4 == 0, at least d rounded up to 128
+ *   h_scale   [rows, lds], lds >= ceil(d / 128)
+ * (metro_op_gemm_fp8 reads h with 16-byte alignment, ldh % 16 == 0, and lds % 4
+ * == 0.)  d % 4 == 0, d <= 8192.  Errors: E_INVAL. */
+metro_status metro_op_rmsnorm_fp8(const float* x, int32_t ldx, const uint16_t* delta, int32_t ldd, const uint16_t* g,
+                                  float eps, float* x_out, uint16_t* h_bf16, int32_t ldh_bf16, uint8_t* h, int32_t ldh,
+                                  uint8_t* h_scale, int32_t lds, int32_t rows, int32_t d, void* stream);
+
+/* Product of 8-bit rows and weights:
+ *   acc[m, n] = sum_b 2^(Ex[m, b] + Ew[n, b] - 254) * sum_{k in b} X[m, k] * W[n, k]
+ * with fp32 accumulators.  (The matrix cores align the products of each eight
+ * columns to the largest and cut them below 2^-13 of it: the error is at most
+ * about 2^-12 sum_k |x w|, 1.5e-5 of the result on normal data.)
+ *   X, x_scale  8-bit rows [M, ldx], [M, ldxs]: the first Kp columns; X 16-byte
+ *               aligned, ldx % 16 == 0; x_scale 4-byte aligned, ldxs % 4 == 0,
+ *               ldxs >= Kp / 128 rounded up to 4
+ *   W, w_scale  as metro_op_pack_weight_fp8 writes them, 16-byte aligned
+ * Kp % 128 == 0, N % 32 == 0.  epilogue:
+ *   0  out_bf16[m*ldo + n] = bf16(acc[m, n]); 8-byte aligned, ldo % 4 == 0, ldo >= N
+ *   2  W rows in blocks of 16 = 8 gate rows then the 8 up rows of the same
+ *      features (as metro_op_gemm): silu(gate) * up as 8-bit rows of N / 2 values
+ *      in out_fp8 [M, ldo] (16-byte aligned, ldo % 16 == 0, ldo >= N / 2 rounded up
+ *      to 128) and out_scale [M, ldos] (ldos >= ceil(N / 256)), rounded from fp32
+ * The other output is NULL.
+ * workspace: NULL, or device fp32 of workspace_bytes, 16-byte aligned: small
+ * products may then run as k slices (ks * M * N floats for ks <= 8 slices where
+ * they fit), summed in slice order.  Which slices run follows from the sizes and
+ * workspace_bytes, so results of equal calls are equal bit for bit.  Outputs
+ * overlap no input.  Errors: E_INVAL. */
+metro_status metro_op_gemm_fp8(const uint8_t* X, int32_t ldx, const uint8_t* x_scale, int32_t ldxs, const uint8_t* W,
+                               const uint8_t* w_scale, int32_t Kp, int32_t M, int32_t N, int32_t epilogue,
+                               uint16_t* out_bf16, uint8_t* out_fp8, int32_t ldo, uint8_t* out_scale, int32_t ldos,
+                               float* workspace, int64_t workspace_bytes, void* stream);
+
+/* Routing of T tokens to top_k of n_experts experts each.  With z = logits[t, :]
+ * and, in fp64, s = softmax(z) (scoring 0) or 1 / (1 + exp(-z)) (scoring 1):
+ *   choice c = s + bias (bias fp32 [n_experts] or NULL; -inf shuts an expert out)
+ *   experts in n_groups equal runs; a group's score is the sum of its two
+ *   largest c (its one c where it has one expert); the top_groups best groups stay
+ *   experts[t, :]  the top_k largest c of theirs, largest first
+ *   weights[t, :]  their s * scale, with renormalise s / sum of the top_k s * scale
+ *                  (0 where that sum is 0)
+ * Ties go to the lowest index.  A NaN choice comes behind every number: where too
+ * few numbers are left, the lowest indices of the staying groups are chosen, so
+ * indices are always distinct and in range.  A row of -inf has s = 0; a NaN or
+ * +inf in a softmax row makes its weights NaN.
+ * And the experts' order of the T * top_k rows, tokens ascending within an expert:
+ *   offsets [n_experts + 1]: expert e has slots offsets[e] .. offsets[e + 1] - 1
+ *   src  [T * top_k]: token of a slot;  slot [T, top_k]: slot of a choice
+ *   logits    device fp32 [T, ldl], ldl >= n_experts (metro_op_gemm's output with
+ *             the router's rows padded to 32 will do)
+ *   experts, src, slot, offsets  device int32;  weights  device fp32
+ *   workspace device int32 of at least 4 * n_experts * ceil(T / 64) bytes; may be
+ *             NULL for T <= 64
+ * 1 <= n_experts <= 512, 1 <= n_groups <= 64, top_k <= 32 and at most the experts of
+ * top_groups groups, T * top_k < 2^31.  Errors: E_INVAL. */
+metro_status metro_op_route(const float* logits, int32_t ldl, const float* bias, int32_t T, int32_t n_experts,
+                            int32_t scoring, int32_t n_groups, int32_t top_groups, int32_t top_k, int32_t renormalise,
+                            float scale, int32_t* experts, float* weights, int32_t* offsets, int32_t* src, int32_t* slot,
+                            int32_t* workspace, int64_t workspace_bytes, void* stream);
+
+/* metro_op_gemm_fp8 by experts: slot m (0 <= m < R) of expert e, offsets[e] <= m <
+ * offsets[e + 1], is row src[m] of X (row m with src NULL) times expert e's weights,
+ *   W + e * N * Kp, w_scale + e * N * G  (each as metro_op_pack_weight_fp8 writes it).
+ *   src       device int32 [R] or NULL: 0 <= src[m] < x_rows
+ *   offsets   device int32 [n_experts + 1], ascending, 0 <= offsets[e] <= R (as
+ *             metro_op_route leaves them)
+ *   x_rows    rows of X; at least R with src NULL
+ * Both are read on the device and held to these ranges there: a row index
+ * outside reads another row of X, and nothing outside the buffers is touched.
+ * Output rows of slots that no expert has are left as they were.  Shapes,
+ * epilogues, alignments, workspace and precision as metro_op_gemm_fp8, with R in
+ * the place of M.  Errors: E_INVAL. */
+metro_status metro_op_gemm_fp8_experts(const uint8_t* X, int32_t ldx, const uint8_t* x_scale, int32_t ldxs,
+                                       int32_t x_rows, const int32_t* src, const int32_t* offsets, int32_t n_experts,
+                                       int32_t R, const uint8_t* W, const uint8_t* w_scale, int32_t Kp, int32_t N,
+                                       int32_t epilogue, uint16_t* out_bf16, uint8_t* out_fp8, int32_t ldo,
+                                       uint8_t* out_scale, int32_t ldos, float* workspace, int64_t workspace_bytes,
+                                       void* stream);
+
+/* The experts' rows back at their tokens:
+ *   out[t, :] = resid[t, :] + sum_j weights[t, j] * y[slot[t, j], :]   (fp32, j ascending)
+ * A slot outside 0 .. y_rows - 1 adds nothing (a choice that was dropped).
+ *   y         device bf16 [y_rows, ldy], 16-byte aligned, ldy % 8 == 0
+ *   weights, slot  device fp32, int32 [T, top_k]
+ *   resid     device fp32 [T, ldo] or NULL (0), 16-byte aligned; may be out
+ *   out       device fp32 [T, ldo], 16-byte aligned, ldo % 4 == 0
+ * d % 8 == 0.  Errors: E_INVAL. */
+metro_status metro_op_combine_experts(const uint16_t* y, int32_t ldy, int32_t y_rows, const float* weights,
+                                      const int32_t* slot, int32_t T, int32_t top_k, int32_t d, const float* resid,
+                                      float* out, int32_t ldo, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

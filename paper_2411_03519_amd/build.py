@@ -29,6 +29,10 @@ SOURCES = [
     "csrc/kernels/elementwise.hip",
     "csrc/kernels/gemm.hip",
     "csrc/kernels/attention.hip",
+    "csrc/ops_fp8.hip",
+    "csrc/kernels/rows_fp8.hip",
+    "csrc/kernels/route.hip",
+    "csrc/kernels/gemm_fp8.hip",
 ]
 
 ARCH = "gfx950"

@@ -1,0 +1,331 @@
+// Routing of tokens to experts (gfx950, wave64): scores, grouped top-k, weights,
+// and the places of the tokens' rows in the experts' order.
+//
+// s = softmax or sigmoid of a token's logits, c = s + bias; of `groups` equal
+// runs of experts the top_groups with the largest sum of their two best c stay;
+// of their experts the k largest c are chosen, ties to the lowest index; weights
+// are their s (over their sum).  Scores are computed in fp64: which of two
+// experts comes first must not hang on the rounding of an exponential, and at
+// E values per token their cost does not show.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "common.h"
+#include "kernels_fp8.h"
+
+namespace metro {
+
+namespace {
+
+// v of another lane of the same 16 (DPP control word), both halves of the double
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_mov_dpp(static_cast<int>(u), CTRL, 0xf, 0xf, true);
+  const uint32_t hi = __builtin_amdgcn_mov_dpp(static_cast<int>(u >> 32), CTRL, 0xf, 0xf, true);
+  return __builtin_bit_cast(double, (static_cast<uint64_t>(hi) << 32) | lo);
+}
+
+// op over the LPT lanes of a token, the result in each of them: pairs, quads,
+// 8 (the mirrored half row), 16 (the mirrored row), then the row swaps.
+template <int LPT, class Op>
+__device__ __forceinline__ double lanes_reduce(double v, Op op) {
+  v = op(v, dpp<0xB1>(v));   // quad_perm 1 0 3 2
+  v = op(v, dpp<0x4E>(v));   // quad_perm 2 3 0 1
+  v = op(v, dpp<0x141>(v));  // row_half_mirror
+  if (LPT >= 16) v = op(v, dpp<0x140>(v));  // row_mirror
+  if (LPT >= 32) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = static_cast<uint32_t>(u), hi = static_cast<uint32_t>(u >> 32);
+    const auto a = __builtin_amdgcn_permlane16_swap(lo, lo, false, false);
+    const auto b = __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+    v = op(__builtin_bit_cast(double, (static_cast<uint64_t>(b[0]) << 32) | a[0]),
+           __builtin_bit_cast(double, (static_cast<uint64_t>(b[1]) << 32) | a[1]));
+  }
+  if (LPT >= 64) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = static_cast<uint32_t>(u), hi = static_cast<uint32_t>(u >> 32);
+    const auto a = __builtin_amdgcn_permlane32_swap(lo, lo, false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
+    v = op(__builtin_bit_cast(double, (static_cast<uint64_t>(b[0]) << 32) | a[0]),
+           __builtin_bit_cast(double, (static_cast<uint64_t>(b[1]) << 32) | a[1]));
+  }
+  return v;
+}
+
+constexpr double kNone = __builtin_nan("");  // an expert that can no longer be chosen
+
+// a score to choose by: a NaN comes behind every number
+__device__ __forceinline__ double choosable(double c) { return c == c ? c : -__builtin_inf(); }
+
+// Scores and choices of the token of this lane's LPT lanes (lane l of them has
+// experts l, l + LPT, ...), t < T valid.  room: LDS of the token, E + 2 * groups
+// doubles (used with groups > 1).  mask: LDS bit sets of the block's tokens, one
+// per expert; bit: the token's.  Every thread of the block calls it.
+template <int LPT, int EPL>
+__device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, bool valid, int l, double* room,
+                                            unsigned long long* mask, int bit) {
+  const float* row = a.logits + (valid ? t : 0) * a.ldl;
+  double s[EPL], c[EPL];
+  int place[EPL];
+  float z[EPL];
+  auto mx = [](double x, double y) { return fmax(x, y); };
+  auto add = [](double x, double y) { return x + y; };
+#pragma unroll
+  for (int q = 0; q < EPL; ++q) {
+    const int e = q * LPT + l;
+    z[q] = e < a.E ? row[e] : -__builtin_inff();
+    place[q] = -1;
+  }
+  if (a.sigmoid) {
+#pragma unroll
+    for (int q = 0; q < EPL; ++q) s[q] = 1.0 / (1.0 + exp(-static_cast<double>(z[q])));
+  } else {
+    double m = z[0];
+#pragma unroll
+    for (int q = 1; q < EPL; ++q) m = fmax(m, static_cast<double>(z[q]));
+    m = lanes_reduce<LPT>(m, mx);
+    double sum = 0.0;
+#pragma unroll
+    for (int q = 0; q < EPL; ++q) {
+      // (a row of nothing but -inf has no scores: all 0)
+      s[q] = z[q] == -__builtin_inff() ? 0.0 : exp(static_cast<double>(z[q]) - m);
+      sum += s[q];
+    }
+    sum = lanes_reduce<LPT>(sum, add);
+    if (sum != 0.0) {
+#pragma unroll
+      for (int q = 0; q < EPL; ++q) s[q] /= sum;
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < EPL; ++q) {
+    const int e = q * LPT + l;
+    c[q] = e < a.E ? choosable(s[q] + (a.bias ? static_cast<double>(a.bias[e]) : 0.0)) : kNone;
+  }
+  if (a.groups > 1) {
+    const int per = a.E / a.groups;
+    double *const best = room + a.E, *const kept = best + a.groups;
+#pragma unroll
+    for (int q = 0; q < EPL; ++q)
+      if (q * LPT + l < a.E) room[q * LPT + l] = c[q];
+    __syncthreads();
+    for (int g = l; g < a.groups; g += LPT) {
+      double first = room[g * per], second = -__builtin_inf();
+      for (int i = 1; i < per; ++i) {
+        const double v = room[g * per + i];
+        second = fmax(second, fmin(first, v));
+        first = fmax(first, v);
+      }
+      best[g] = choosable(per > 1 ? first + second : first);
+    }
+    __syncthreads();
+    for (int g = l; g < a.groups; g += LPT) {
+      int ahead = 0;
+      for (int i = 0; i < a.groups; ++i) ahead += best[i] > best[g] || (best[i] == best[g] && i < g);
+      kept[g] = ahead < a.top_groups ? 1.0 : 0.0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < EPL; ++q) {
+      const int e = q * LPT + l;
+      if (e < a.E && kept[e / per] == 0.0) c[q] = kNone;
+    }
+  }
+  const int shift = (threadIdx.x & 63) / LPT * LPT;
+  for (int j = 0; j < a.k; ++j) {
+    double m = c[0];
+#pragma unroll
+    for (int q = 1; q < EPL; ++q) m = fmax(m, c[q]);
+    m = lanes_reduce<LPT>(m, mx);
+    bool found = false;
+#pragma unroll
+    for (int q = 0; q < EPL; ++q) {
+      const uint64_t bits = (__ballot(c[q] == m) >> shift) & (~0ull >> (64 - LPT));
+      if (!found && bits) {
+        found = true;
+        if (l == __builtin_ctzll(bits)) {
+          place[q] = j;
+          c[q] = kNone;
+        }
+      }
+    }
+  }
+  double sum = 0.0;
+#pragma unroll
+  for (int q = 0; q < EPL; ++q)
+    if (place[q] >= 0) sum += s[q];
+  sum = lanes_reduce<LPT>(sum, add);
+  const double by = a.renormalise && sum != 0.0 ? a.scale / sum : a.scale;
+#pragma unroll
+  for (int q = 0; q < EPL; ++q)
+    if (valid && place[q] >= 0) {
+      const int e = q * LPT + l;
+      a.experts[t * a.k + place[q]] = e;
+      a.weights[t * a.k + place[q]] = static_cast<float>(s[q] * by);
+      atomicOr(&mask[e], 1ull << bit);
+    }
+}
+
+// exclusive prefix sum of n <= kRouteMaxExperts counts in LDS by one workgroup;
+// the total behind them (v has n + 1 places)
+template <int NTH>
+__device__ __forceinline__ void prefix(int32_t* v, int n, int32_t* wave_sums) {
+  int carry = 0;
+  for (int i0 = 0; i0 < n; i0 += NTH) {
+    const int i = i0 + threadIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int own = i < n ? v[i] : 0;
+    int x = own;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const int y = __shfl_up(x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 63) wave_sums[w] = x;
+    __syncthreads();
+    int before = carry, total = carry;
+    for (int k = 0; k < NTH / 64; ++k) {
+      if (k < w) before += wave_sums[k];
+      total += wave_sums[k];
+    }
+    if (i < n) v[i] = before + x - own;
+    carry = total;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) v[n] = carry;
+  __syncthreads();
+}
+
+// Choices of kRouteBlock tokens.  ALONE: they are all there are, and the block
+// finds their places too; else it leaves its count of each expert in ws.
+template <int NTH, int LPT, int EPL, bool ALONE>
+__global__ __launch_bounds__(NTH) void route_kernel(RouteArgs a) {
+  extern __shared__ double room[];
+  __shared__ unsigned long long mask[kRouteMaxExperts];
+  __shared__ int32_t base[kRouteMaxExperts + 1], wave_sums[NTH / 64];
+  for (int e = threadIdx.x; e < a.E; e += NTH) mask[e] = 0;
+  __syncthreads();
+  constexpr int kPerPass = NTH / LPT;
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRouteBlock;
+  const int n = static_cast<int>(min(static_cast<int64_t>(kRouteBlock), a.T - t0));
+  const int mine = threadIdx.x / LPT;
+  for (int i0 = 0; i0 < n; i0 += kPerPass) {
+    const int i = i0 + mine;
+    route_token<LPT, EPL>(a, t0 + i, i < n, threadIdx.x % LPT, room + mine * (a.E + 2 * a.groups), mask, i);
+  }
+  __syncthreads();
+  if (!ALONE) {
+    for (int e = threadIdx.x; e < a.E; e += NTH)
+      a.ws[static_cast<int64_t>(e) * gridDim.x + blockIdx.x] = __popcll(mask[e]);
+    return;
+  }
+  for (int e = threadIdx.x; e < a.E; e += NTH) base[e] = __popcll(mask[e]);
+  __syncthreads();
+  prefix<NTH>(base, a.E, wave_sums);
+  for (int e = threadIdx.x; e <= a.E; e += NTH) a.offsets[e] = base[e];
+  for (int u = threadIdx.x; u < n * a.k; u += NTH) {
+    const int e = a.experts[u], i = u / a.k;
+    const int sl = base[e] + __popcll(mask[e] & ((1ull << i) - 1));
+    a.slot[u] = sl;
+    a.src[sl] = i;
+  }
+}
+
+// ws[e][b]: counts of block b -> counts of blocks 0 .. b
+__global__ __launch_bounds__(256) void route_scan_kernel(int32_t* ws, int nb) {
+  __shared__ int32_t wave_sums[4];
+  int32_t* v = ws + static_cast<int64_t>(blockIdx.x) * nb;
+  int carry = 0;
+  for (int i0 = 0; i0 < nb; i0 += 256) {
+    const int i = i0 + threadIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    int x = i < nb ? v[i] : 0;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const int y = __shfl_up(x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 63) wave_sums[w] = x;
+    __syncthreads();
+    int before = carry;
+    for (int k = 0; k < 4; ++k) {
+      if (k < w) before += wave_sums[k];
+      carry += wave_sums[k];
+    }
+    if (i < nb) v[i] = before + x;
+    __syncthreads();
+  }
+}
+
+// Places of a block's tokens: the rows of its experts before it, then its own
+// tokens in order.
+__global__ __launch_bounds__(256) void route_place_kernel(RouteArgs a, int nb) {
+  __shared__ unsigned long long mask[kRouteMaxExperts];
+  __shared__ int32_t base[kRouteMaxExperts + 1], wave_sums[4];
+  const int b = blockIdx.x;
+  const int64_t t0 = static_cast<int64_t>(b) * kRouteBlock;
+  const int n = static_cast<int>(min(static_cast<int64_t>(kRouteBlock), a.T - t0));
+  for (int e = threadIdx.x; e < a.E; e += 256) {
+    mask[e] = 0;
+    base[e] = a.ws[static_cast<int64_t>(e) * nb + nb - 1];
+  }
+  __syncthreads();
+  prefix<256>(base, a.E, wave_sums);
+  if (b == 0)
+    for (int e = threadIdx.x; e <= a.E; e += 256) a.offsets[e] = base[e];
+  for (int u = threadIdx.x; u < n * a.k; u += 256) atomicOr(&mask[a.experts[t0 * a.k + u]], 1ull << (u / a.k));
+  __syncthreads();
+  if (b > 0)
+    for (int e = threadIdx.x; e < a.E; e += 256) base[e] += a.ws[static_cast<int64_t>(e) * nb + b - 1];
+  __syncthreads();
+  for (int u = threadIdx.x; u < n * a.k; u += 256) {
+    const int e = a.experts[t0 * a.k + u], i = u / a.k;
+    const int sl = base[e] + __popcll(mask[e] & ((1ull << i) - 1));
+    a.slot[t0 * a.k + u] = sl;
+    a.src[sl] = static_cast<int32_t>(t0 + i);
+  }
+}
+
+template <int NTH, bool ALONE>
+void launch_choices(const RouteArgs& a, int nb, hipStream_t s) {
+  auto go = [&](auto lpt, auto epl) {
+    constexpr int LPT = decltype(lpt)::value, EPL = decltype(epl)::value;
+    const uint32_t room = a.groups > 1 ? static_cast<uint32_t>(NTH / LPT * (a.E + 2 * a.groups) * sizeof(double)) : 0;
+    route_kernel<NTH, LPT, EPL, ALONE><<<dim3(nb), dim3(NTH), room, s>>>(a);
+  };
+  using std::integral_constant;
+  if (a.E <= 8)
+    go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+  else if (a.E <= 16)
+    go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+  else if (a.E <= 32)
+    go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+  else if (a.E <= 64)
+    go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  else if (a.E <= 128)
+    go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  else if (a.E <= 256)
+    go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  else
+    go(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+}
+
+}  // namespace
+
+hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
+  if (a.T <= kRouteBlock) {
+    launch_choices<512, true>(a, 1, s);
+    return hipGetLastError();
+  }
+  const int nb = (a.T + kRouteBlock - 1) / kRouteBlock;
+  launch_choices<256, false>(a, nb, s);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  route_scan_kernel<<<dim3(a.E), dim3(256), 0, s>>>(a.ws, nb);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  route_place_kernel<<<dim3(nb), dim3(256), 0, s>>>(a, nb);
+  return hipGetLastError();
+}
+
+}  // namespace metro

@@ -82,6 +82,16 @@ _SIGS = {
     "metro_op_attn_decode": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp]),
     "metro_op_attn_prefill": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp]),
     "metro_op_attn_decode_noalloc": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp]),
+    "metro_op_pack_weight_fp8": (_i32, [_vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp]),
+    "metro_op_rmsnorm_fp8": (_i32, [_vp, _i32, _vp, _i32, _vp, ctypes.c_float, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _i32,
+                                    _i32, _vp]),
+    "metro_op_gemm_fp8": (_i32, [_vp, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _i32, _vp, _i32, _vp,
+                                 _i64, _vp]),
+    "metro_op_route": (_i32, [_vp, _i32, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, ctypes.c_float, _vp, _vp, _vp, _vp,
+                              _vp, _vp, _i64, _vp]),
+    "metro_op_gemm_fp8_experts": (_i32, [_vp, _i32, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32, _vp,
+                                         _vp, _i32, _vp, _i32, _vp, _i64, _vp]),
+    "metro_op_combine_experts": (_i32, [_vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _i32, _vp]),
     "metro_sched_create": (_i32, [_vp, _vp, ctypes.POINTER(_vp)]),
     "metro_sched_destroy": (None, [_vp]),
     "metro_sched_next": (_i32, [_vp, ctypes.POINTER(_i32), ctypes.POINTER(_i32), _vp, _i32, ctypes.POINTER(_i32)]),
@@ -337,6 +347,84 @@ def op_attn_prefill(q, kv, n_pages: int, nq: int, nkv: int, hd: int, cu_q, ctx_b
     bt = _host_i32(block_tables)
     check(lib.metro_op_attn_prefill(_ptr(q), _ptr(kv), n_pages, nq, nkv, hd, len(cb), cu.ctypes.data,
                                     cb.ctypes.data, bt.ctypes.data, _ptr(out), _stream(stream)))
+
+
+# -- 8-bit feed-forward (see metro_ops.h); codes and scales are uint8 tensors ------
+
+EPI_FP8_BF16, EPI_FP8_SWIGLU = 0, 2
+SOFTMAX, SIGMOID = 0, 1
+
+
+def _bytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def _pad(n: int, to: int) -> int:
+    return -(-n // to) * to
+
+
+def op_pack_weight_fp8(W, ld: int, N: int, K: int, Kp: int, out, scale, stream=None):
+    """Row-major bf16 W [N, ld] (first K columns) -> out, the [N, Kp] codes, and
+    scale, their E8M0 bytes, as op_gemm_fp8 reads them."""
+    check(lib.metro_op_pack_weight_fp8(_ptr(W), ld, N, K, Kp, _ptr(out), _ptr(scale), _stream(stream)))
+
+
+def op_rmsnorm_fp8(x, g, eps: float, h, h_scale, rows: int, d: int, delta=None, x_out=None, h_bf16=None,
+                   ldx: int | None = None, ldd: int | None = None, ldh_bf16: int | None = None, ldh: int | None = None,
+                   lds: int | None = None, stream=None):
+    """x (+ bf16 delta -> x_out) -> 8-bit rows h, h_scale (and bf16 rows h_bf16).
+    Strides default to d, d rounded up to 128 (ldh) and its groups rounded up to
+    4 (lds)."""
+    check(lib.metro_op_rmsnorm_fp8(_ptr(x), d if ldx is None else ldx, _ptr(delta), d if ldd is None else ldd, _ptr(g),
+                                   eps, _ptr(x_out), _ptr(h_bf16), d if ldh_bf16 is None else ldh_bf16, _ptr(h),
+                                   _pad(d, 128) if ldh is None else ldh, _ptr(h_scale),
+                                   _pad(_pad(d, 128) // 128, 4) if lds is None else lds, rows, d, _stream(stream)))
+
+
+def _gemm_fp8_out(epilogue: int, out, N: int, ldo, ldos):
+    swiglu = epilogue == EPI_FP8_SWIGLU
+    cols = _pad(N // 2, 128) if swiglu else N
+    return (None if swiglu else _ptr(out), _ptr(out) if swiglu else None, cols if ldo is None else ldo,
+            _pad(cols // 128, 4) if ldos is None else ldos)
+
+
+def op_gemm_fp8(X, x_scale, W, w_scale, M: int, N: int, Kp: int, epilogue: int, out, out_scale=None,
+                ldx: int | None = None, ldxs: int | None = None, ldo: int | None = None, ldos: int | None = None,
+                workspace=None, stream=None):
+    """8-bit rows X times packed W -> out: bf16 rows (EPI_FP8_BF16), or the 8-bit
+    rows of SwiGLU with out_scale (EPI_FP8_SWIGLU)."""
+    o16, o8, ldo, ldos = _gemm_fp8_out(epilogue, out, N, ldo, ldos)
+    check(lib.metro_op_gemm_fp8(_ptr(X), Kp if ldx is None else ldx, _ptr(x_scale),
+                                _pad(Kp // 128, 4) if ldxs is None else ldxs, _ptr(W), _ptr(w_scale), Kp, M, N, epilogue,
+                                o16, o8, ldo, _ptr(out_scale), ldos, _ptr(workspace), _bytes(workspace),
+                                _stream(stream)))
+
+
+def op_route(logits, T: int, n_experts: int, top_k: int, experts, weights, offsets, src, slot, bias=None,
+             ldl: int | None = None, scoring: int = SOFTMAX, n_groups: int = 1, top_groups: int = 1,
+             renormalise: bool = True, scale: float = 1.0, workspace=None, stream=None):
+    """Top experts of each token, their weights, and the experts' order of the rows."""
+    check(lib.metro_op_route(_ptr(logits), n_experts if ldl is None else ldl, _ptr(bias), T, n_experts, scoring, n_groups,
+                             top_groups, top_k, int(bool(renormalise)), scale, _ptr(experts), _ptr(weights),
+                             _ptr(offsets), _ptr(src), _ptr(slot), _ptr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def op_gemm_fp8_experts(X, x_scale, x_rows: int, src, offsets, n_experts: int, R: int, W, w_scale, N: int, Kp: int,
+                        epilogue: int, out, out_scale=None, ldx: int | None = None, ldxs: int | None = None,
+                        ldo: int | None = None, ldos: int | None = None, workspace=None, stream=None):
+    """op_gemm_fp8 of each expert's slots with its own weights (src None: slot m is row m of X)."""
+    o16, o8, ldo, ldos = _gemm_fp8_out(epilogue, out, N, ldo, ldos)
+    check(lib.metro_op_gemm_fp8_experts(_ptr(X), Kp if ldx is None else ldx, _ptr(x_scale),
+                                        _pad(Kp // 128, 4) if ldxs is None else ldxs, x_rows, _ptr(src), _ptr(offsets),
+                                        n_experts, R, _ptr(W), _ptr(w_scale), Kp, N, epilogue, o16, o8, ldo,
+                                        _ptr(out_scale), ldos, _ptr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def op_combine_experts(y, y_rows: int, weights, slot, T: int, top_k: int, d: int, out, resid=None,
+                       ldy: int | None = None, ldo: int | None = None, stream=None):
+    """out = resid + the weighted sum of each token's slots of y."""
+    check(lib.metro_op_combine_experts(_ptr(y), d if ldy is None else ldy, y_rows, _ptr(weights), _ptr(slot), T, top_k, d,
+                                       _ptr(resid), _ptr(out), d if ldo is None else ldo, _stream(stream)))
 
 
 # ----------------------------------------------------------------------------
