@@ -14,6 +14,7 @@
 // a product of normals), against 1.7e-3 that the rounding to bf16 adds behind it.
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "fp8.h"
 #include "kernels_fp8.h"
@@ -30,7 +31,13 @@ __device__ __forceinline__ f32x4 mfma8(uint4 a0, uint4 a1, uint4 b0, uint4 b1, f
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, sa, 0, sb);
 }
 
-__device__ __forceinline__ float silu_f32(float z) { return z / (1.0f + expf(-z)); }
+// z / (1 + exp(-z)) by the hardware's 2^x and reciprocal (an ulp each; the
+// product with log2(e) is off by |z| / 2 ulp of the exponent's result): far below
+// the step of the e4m3 value that it ends in, at a fifth of expf's and the
+// division's instructions.
+__device__ __forceinline__ float silu_f32(float z) {
+  return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+}
 
 // Rows m0 .. m1 - 1 of row block b of BM rows, and their expert.  By experts,
 // every expert's rows are cut into blocks of their own; offsets are held within
@@ -69,9 +76,399 @@ __device__ __forceinline__ bool row_block(const GemmFp8Args& a, int b, int BM, i
   return false;
 }
 
+// all row blocks of BM rows
+__device__ __forceinline__ int total_row_blocks(const GemmFp8Args& a, int BM) {
+  if (!a.offsets) return (a.M + BM - 1) / BM;
+  const int lane = threadIdx.x & 63;
+  int n = 0;
+  for (int i = lane; i < a.E; i += 64) {
+    const int lo = min(max(a.offsets[i], 0), a.M), hi = min(max(a.offsets[i + 1], 0), a.M);
+    n += (max(hi - lo, 0) + BM - 1) / BM;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
+  return __builtin_amdgcn_readfirstlane(n);
+}
+
 // row of X that slot m reads (indexes are held within x_rows)
 __device__ __forceinline__ int64_t source_row(const GemmFp8Args& a, int m) {
   return a.src ? min(max(a.src[m], 0), a.x_rows - 1) : m;
+}
+
+// ---------------------------------------------------------------------------
+// Tiled kernel: 4 waves, one per SIMD (2 x 2, each 16 TN rows of W x 16 TM rows of
+// X); operands come through LDS in stages of 128 columns, one per instruction.
+//
+// A stage's work is cut in two halves of TN / 2 row tiles of W.  LDS rings hold
+// chunks: the W rows of one half (of both wave rows), and half the X rows of a
+// stage.  During half h = 2 s + p the wave multiplies from registers, reads the W
+// fragments of half h + 1 and half of the X fragments of stage s + 1 (chunk h + 2),
+// and requests chunk h + 5 of both, into slots whose last reads lie behind the
+// previous barrier (W ring 5 chunks, X ring 4).  The barrier that ends the half
+// stands for: W chunk h + 2 and X chunk h + 3 have landed, and what this half read
+// is in registers.  Every memory instruction rides behind a matrix instruction.
+// Scales: four stages' bytes of a row are one word; they have a ring of their
+// own of two groups of four stages, requested four stages ahead.
+// ---------------------------------------------------------------------------
+template <int TN_, int TM_>
+struct TileShape8 {
+  static constexpr int TN = TN_, TM = TM_;
+  static constexpr int BN = 32 * TN, BM = 32 * TM;
+  static constexpr int WR = 5, XR = 4;
+  static constexpr int kW = TN * 2048, kX = TM * 2048;  // bytes of a chunk
+  static constexpr int LW = TN / 2, LX = TM / 2;        // wave loads of a chunk, per wave
+  static constexpr int kScales = 4 * (BN + BM);         // bytes of a group of four stages
+  static constexpr int kLds = WR * kW + XR * kX + 2 * kScales;
+  static constexpr int OCC = kLds <= 80 * 1024 ? 2 : 1;
+  static_assert(TN % 4 == 0 && TM % 2 == 0, "halves and fragments are shared evenly");
+};
+
+// c += a . b scaled by 2^(sa - 127 + sb - 127) (lowest bytes), the accumulator in
+// place.  The compiler does not see these instructions' hazards: no operand is
+// written by a vector instruction within two wait states of one, and the
+// accumulators are read behind drained_barrier.
+__device__ __forceinline__ void mfma8_acc(f32x4& c, i32x8 a, i32x8 b, int sa, int sb) {
+  asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]"
+               : "+a"(c)
+               : "v"(a), "v"(b), "v"(sa), "v"(sb));
+}
+// The same with a direct load of 16 bytes per lane into LDS bytes lds_base + INC +
+// 16 * lane behind it; the matrix instruction is the wait state between the M0
+// write and the load.
+template <int INC>
+__device__ __forceinline__ void mfma8_acc_load(f32x4& c, i32x8 a, i32x8 b, int sa, int sb, const void* base,
+                                               uint32_t off, uint32_t lds_base) {
+  asm volatile(
+      "s_add_u32 m0, %5, %6\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]\n\t"
+      "global_load_lds_dwordx4 %7, %8"
+      : "+a"(c)
+      : "v"(a), "v"(b), "v"(sa), "v"(sb), "s"(lds_base), "n"(INC), "v"(off), "s"(base)
+      : "memory", "m0", "scc");
+}
+// 4 bytes per lane into LDS bytes lds_base + 4 * lane
+__device__ __forceinline__ void lds_load4s(const void* base, uint32_t off, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds_base)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void drained_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_nop 7\n\ts_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// first of the n memory operations that ride behind instruction u of nm, spread
+// evenly (those before instruction u: first_of(u + 1) is the end of its own)
+constexpr int first_of(int u, int nm, int n) { return (u * n + nm - 1) / nm; }
+
+// Work item of workgroup b (of `total`) such that each of the 8 XCDs, which take
+// workgroups in turn and have an L2 each, gets a contiguous run of the list.
+__device__ __forceinline__ int xcd_run(int b, int total) {
+  constexpr int kXcds = 8;
+  const int q = total / kXcds, r = total % kXcds, x = b % kXcds, s = b / kXcds;
+  return x * q + min(x, r) + s;
+}
+
+// Tile t of mb row blocks x nb column tiles: groups of GM row blocks, rows
+// fastest within a group, so that tiles in flight share X and W tiles.
+template <int GM>
+__device__ __forceinline__ void tile_at(int t, int mb, int nb, int& bm, int& bn) {
+  const int group = t / (GM * nb), first = group * GM, gm = min(mb - first, GM), in = t % (GM * nb);
+  bn = in / gm;
+  bm = first + in % gm;
+}
+
+// 4 x 4 transposition of words over the lanes r + 16 g: word p of lane group g
+// becomes word g of lane group p
+__device__ __forceinline__ void transpose4(uint32_t (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const auto t = __builtin_amdgcn_permlane32_swap(v[i], v[i + 2], false, false);
+    v[i] = t[0];
+    v[i + 2] = t[1];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; i += 2) {
+    const auto t = __builtin_amdgcn_permlane16_swap(v[i], v[i + 1], false, false);
+    v[i] = t[0];
+    v[i + 1] = t[1];
+  }
+}
+
+template <class S, int EPI>
+__global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args a) {
+  constexpr int TN = S::TN, TM = S::TM, HN = TN / 2, HM = TM / 2, LW = S::LW, LX = S::LX;
+  __shared__ uint4 lds[S::kLds / 16];
+  const int nb = (a.N + S::BN - 1) / S::BN;
+  const int mb = total_row_blocks(a, S::BM);
+  if (static_cast<int>(blockIdx.x) >= mb * nb) return;
+  int bm, bn, e, m0, m1;
+  tile_at<4>(xcd_run(blockIdx.x, mb * nb), mb, nb, bm, bn);
+  if (!row_block(a, bm, S::BM, e, m0, m1)) return;
+  e = __builtin_amdgcn_readfirstlane(e);
+  m0 = __builtin_amdgcn_readfirstlane(m0);
+  m1 = __builtin_amdgcn_readfirstlane(m1);
+  const int n0 = bn * S::BN;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wn = wave >> 1, wm = wave & 1;
+  const int r16 = lane & 15, g = lane >> 4;
+  const int nk = a.Kp / kGroup, groups = padded_groups(a.Kp);
+
+  // Loads of a chunk: W chunk p of a stage has tiles wn' * HN + i of wave row wn',
+  // two KiB halves each; X chunk p has rows 16 (wm' TM + p HM) .. of wave column
+  // wm', in blocks of 8.  Tiles and rows past the ends re-read the last ones,
+  // whose products only reach outputs that are not stored.
+  const char* const wbase = reinterpret_cast<const char*>(a.W) + static_cast<int64_t>(e) * a.N * a.Kp +
+                            static_cast<int64_t>(n0) * a.Kp;
+  const int64_t xrow0 = a.src ? 0 : m0;
+  const char* const xbase = reinterpret_cast<const char*>(a.X) + xrow0 * a.ldx;
+  uint32_t woff[2][LW], xoff[2][LX];
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+#pragma unroll
+    for (int j = 0; j < LW; ++j) {
+      const int u = wave * LW + j, t = u >> 1;  // half-tile u of 2 TN
+      const int tile = min((t / HN) * TN + p * HN + t % HN, a.N / 16 - 1 - n0 / 16);
+      woff[p][j] = static_cast<uint32_t>(tile) * (a.Kp * 16) + (u & 1) * 1024 + lane * 16;
+    }
+#pragma unroll
+    for (int j = 0; j < LX; ++j) {
+      const int u = wave * LX + j, t = u >> 1;  // block of 8 rows u of 2 TM
+      const int row = 16 * ((t / HM) * TM + p * HM + t % HM) + 8 * (u & 1) + (lane >> 3);
+      const int m = min(m0 + row, m1 - 1);
+      xoff[p][j] = static_cast<uint32_t>(source_row(a, m) - xrow0) * static_cast<uint32_t>(a.ldx) +
+                   16 * ((lane & 7) ^ (lane >> 3));
+    }
+  }
+  const uint32_t lds0 = lds_address(lds);
+  constexpr uint32_t kXAt = S::WR * S::kW, kSAt = kXAt + S::XR * S::kX;
+  const uint32_t wdst = lds0 + wave * LW * 1024, xdst = lds0 + kXAt + wave * LX * 1024;
+  // scales: a wave loads words of 64 W rows and of 64 X rows of a group
+  const char* const wsbase = reinterpret_cast<const char*>(a.w_scale) + static_cast<int64_t>(e) * a.N * groups;
+  const char* const xsbase = reinterpret_cast<const char*>(a.x_scale) + xrow0 * a.ldxs;
+  const int ws64 = wave % (S::BN / 64), xs64 = wave % (S::BM / 64);
+  const uint32_t wsoff = static_cast<uint32_t>(min(n0 / 16 + ws64 * 4 + g, a.N / 16 - 1)) * (groups * 16) + r16 * 4;
+  const uint32_t xsoff = static_cast<uint32_t>(source_row(a, min(m0 + xs64 * 64 + lane, m1 - 1)) - xrow0) *
+                         static_cast<uint32_t>(a.ldxs);
+  auto load_scales = [&](int q) __attribute__((always_inline)) {  // group q (at most the last)
+    const int at = min(q, groups / 4 - 1);
+    const uint32_t slot = lds0 + kSAt + (q & 1) * S::kScales;
+    lds_load4s(wsbase + at * 64, wsoff, slot + ws64 * 256);
+    lds_load4s(xsbase + at * 4, xsoff, slot + S::BN * 4 + xs64 * 256);
+  };
+
+  f32x4 acc[TN][TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const char* const ldsb = reinterpret_cast<const char*>(lds);
+  const uint32_t wfrag = wn * HN * 2048 + lane * 16;
+  const uint32_t xfrag = kXAt + wm * HM * 2048 + (r16 >> 3) * 1024 + (r16 & 7) * 128 + 16 * (g ^ (r16 & 7));
+  union Frag {
+    uint4 half[2];
+    i32x8 all;
+  };
+  Frag fa[2][HN], fb[2][TM];
+  int sw[TN], sx[TM];
+  // W tile i of the chunk at ring offset wo; X tile j of the chunk at xo
+  auto read_a = [&](Frag (&to)[HN], int u, uint32_t wo) __attribute__((always_inline)) {
+    to[u >> 1].half[u & 1] = *reinterpret_cast<const uint4*>(ldsb + (wfrag + wo) + u * 1024);
+  };
+  auto read_b = [&](Frag& to, int h, int j, uint32_t xo) __attribute__((always_inline)) {
+    to.half[h] = *reinterpret_cast<const uint4*>(ldsb + ((xfrag ^ (64 * h)) + xo) + j * 2048);
+  };
+  auto read_scales = [&](int q) __attribute__((always_inline)) {
+    const uint32_t slot = kSAt + (q & 1) * S::kScales;
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+      sw[i] = *reinterpret_cast<const int*>(ldsb + slot + ((wn * TN + i) * 16 + r16) * 4);
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+      sx[j] = *reinterpret_cast<const int*>(ldsb + slot + S::BN * 4 + ((wm * TM + j) * 16 + r16) * 4);
+  };
+  auto stage_at = [&](int c) __attribute__((always_inline)) { return min(c >> 1, nk - 1); };
+  auto load_w = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < LW; ++j)
+      lds_load16s(wbase + stage_at(c) * 2048, woff[c & 1][j], wdst + (c % S::WR) * S::kW + j * 1024);
+  };
+  auto load_x = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < LX; ++j)
+      lds_load16s(xbase + stage_at(c) * kGroup, xoff[c & 1][j], xdst + (c % S::XR) * S::kX + j * 1024);
+  };
+
+  load_scales(0);
+  load_x(0);
+  load_x(1);
+  load_w(0);
+  load_w(1);
+  load_x(2);
+  load_w(2);
+  load_x(3);
+  load_w(3);
+  wait_vmcnt<3 * LW + 2 * LX>();
+  lds_barrier();
+#pragma unroll
+  for (int u = 0; u < TN; ++u) read_a(fa[0], u, 0);
+#pragma unroll
+  for (int j = 0; j < TM; ++j)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) read_b(fb[0][j], h, j % HM, (j / HM) * S::kX);
+  read_scales(0);
+  drained_barrier();
+  load_x(4);
+  load_w(4);
+  wait_vmcnt<3 * LW + 2 * LX>();
+  drained_barrier();
+
+  // One half: P parity of the stage, H half; its W fragments are fa[H].  wo, xo:
+  // ring offsets of the chunks to read; wsrc .. xd: sources and places of the
+  // chunks to request.
+  auto half = [&](auto par, auto hlf, uint32_t wo, uint32_t xo, const char* wsrc, uint32_t wd, const char* xsrc,
+                  uint32_t xd) __attribute__((always_inline)) {
+    constexpr int P = decltype(par)::value, H = decltype(hlf)::value, NM = HN * TM, ND = LW + LX, NR = TN + TM;
+    // direct loads behind the odd instructions of NM, or where they are many of any
+    constexpr int kSlots = 2 * ND <= NM ? NM / 2 : NM;
+    static_assert(ND <= NM, "at most one direct load behind an instruction");
+    [&]<int... U>(std::integer_sequence<int, U...>) __attribute__((always_inline)) {
+      (([&]() __attribute__((always_inline)) {
+         constexpr int i = U / TM, j = (i & 1) ? TM - 1 - U % TM : U % TM;
+         constexpr int slot = kSlots == NM ? U : U / 2;
+         constexpr bool takes = kSlots == NM || U % 2 == 1;
+         constexpr int l = takes && first_of(slot, kSlots, ND) < first_of(slot + 1, kSlots, ND) ? first_of(slot, kSlots, ND) : ND;
+         f32x4& c = acc[H * HN + i][j];
+         // chunks h + 5: the other half's
+         if constexpr (l < LX)
+           mfma8_acc_load<l * 1024>(c, fa[H][i].all, fb[P][j].all, sw[H * HN + i], sx[j], xsrc, xoff[H ^ 1][l], xd);
+         else if constexpr (l < ND)
+           mfma8_acc_load<(l - LX) * 1024>(c, fa[H][i].all, fb[P][j].all, sw[H * HN + i], sx[j], wsrc,
+                                           woff[H ^ 1][l - LX], wd);
+         else
+           mfma8_acc(c, fa[H][i].all, fb[P][j].all, sw[H * HN + i], sx[j]);
+#pragma unroll
+         for (int u = first_of(U, NM, NR); u < first_of(U + 1, NM, NR); ++u) {
+           if (u < TN)
+             read_a(fa[H ^ 1], u, wo);
+           else
+             read_b(fb[P ^ 1][H * HM + (u - TN) / 2], (u - TN) % 2, (u - TN) / 2, xo);
+         }
+         __builtin_amdgcn_sched_barrier(0);
+       }()),
+       ...);
+    }(std::make_integer_sequence<int, NM>{});
+    wait_vmcnt<3 * LW + 2 * LX>();
+  };
+  // ring offsets of chunk h + 1 (W) and h + 2 (X) to read; of chunk h + 5: W's slot is that of h, X's that of h + 1
+  uint32_t w_read = S::kW, w_put = 0, x_read = 2 * S::kX, x_put = S::kX;
+  auto turn = [&]() __attribute__((always_inline)) {
+    w_put = w_read;
+    w_read = w_read + S::kW == S::WR * S::kW ? 0 : w_read + S::kW;
+    x_put = x_read;
+    x_read = x_read + S::kX == S::XR * S::kX ? 0 : x_read + S::kX;
+  };
+  auto stage = [&](auto par, int s) __attribute__((always_inline)) {
+    if ((s & 3) == 0) load_scales((s >> 2) + 1);
+    const int s0 = min(s + 2, nk - 1), s1 = min(s + 3, nk - 1);
+    half(par, std::integral_constant<int, 0>{}, w_read, x_read, wbase + s0 * 2048, wdst + w_put, xbase + s0 * kGroup,
+         xdst + x_put);
+    turn();
+    drained_barrier();
+    half(par, std::integral_constant<int, 1>{}, w_read, x_read, wbase + s1 * 2048, wdst + w_put, xbase + s1 * kGroup,
+         xdst + x_put);
+    turn();
+    if (s + 1 >= nk) {
+      // a stage behind an odd last one repeats its columns with both powers
+      // 2^-127, in which every product is below the least fp32 value
+#pragma unroll
+      for (int i = 0; i < TN; ++i) sw[i] = 0;
+#pragma unroll
+      for (int j = 0; j < TM; ++j) sx[j] = 0;
+    } else if ((s & 3) == 3) {
+      read_scales((s >> 2) + 1);
+    } else {
+#pragma unroll
+      for (int i = 0; i < TN; ++i) sw[i] = static_cast<uint32_t>(sw[i]) >> 8;
+#pragma unroll
+      for (int j = 0; j < TM; ++j) sx[j] = static_cast<uint32_t>(sx[j]) >> 8;
+    }
+    drained_barrier();
+  };
+  for (int s = 0; s < nk; s += 2) {
+    stage(std::integral_constant<int, 0>{}, s);
+    stage(std::integral_constant<int, 1>{}, s + 1);
+  }
+  wait_vmcnt<0>();
+  drained_barrier();
+
+  const int mw = m0 + wm * 16 * TM, nw = n0 + wn * 16 * TN;
+  if constexpr (EPI == kEpi8Bf16) {
+    // four tiles' words are transposed over the lane groups, so that a lane has
+    // the 16 columns of one tile and four lanes a whole line of a row
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int m = mw + 16 * j + r16;
+#pragma unroll
+      for (int i = 0; i < TN; i += 4) {
+        uint32_t lo[4], hi[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          lo[t] = pack_bf16x2(acc[i + t][j][0], acc[i + t][j][1]);
+          hi[t] = pack_bf16x2(acc[i + t][j][2], acc[i + t][j][3]);
+        }
+        transpose4(lo);
+        transpose4(hi);
+        const int n = nw + 16 * (i + g);
+        if (m < m1 && n < a.N) {
+          uint2* o = reinterpret_cast<uint2*>(a.out16 + static_cast<int64_t>(m) * a.ldo + n);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) o[t] = make_uint2(lo[t], hi[t]);  // (rows are 8-byte aligned)
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  } else {
+    static_assert(S::BN == 256, "a workgroup has a group of 128 features");
+    float* const top = reinterpret_cast<float*>(lds);  // [2][BM]
+    f32x4 y[TM][HN];
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      float best = 0.f;
+#pragma unroll
+      for (int p = 0; p < HN; ++p) {
+        f32x4 gate, up;
+        gate_and_up(acc[2 * p][j], acc[2 * p + 1][j], gate, up);
+        const bool in = nw + 32 * p < a.N;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          y[j][p][i] = in ? silu_f32(gate[i]) * up[i] : 0.f;
+          best = fmaxf(best, fabsf(y[j][p][i]));
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      best = max_xor32(max_xor16(best));
+      if (g == 0) top[wn * S::BM + (wm * TM + j) * 16 + r16] = best;
+    }
+    __syncthreads();
+    const int F = a.N / 2, f = nw / 2 + 16 * g;
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int m = mw + 16 * j + r16, at = (wm * TM + j) * 16 + r16;
+      const int ex = e8m0_of(fmaxf(top[at], top[S::BM + at]));
+      const float s = e8m0_inverse(ex);
+      uint32_t c[4];
+#pragma unroll
+      for (int p = 0; p < 4; ++p) c[p] = pack_e4m3(y[j][p][0] * s, y[j][p][1] * s, y[j][p][2] * s, y[j][p][3] * s);
+      transpose4(c);
+      if (m < m1) {
+        if (f < (F + kGroup - 1) / kGroup * kGroup)
+          *reinterpret_cast<uint4*>(a.out8 + static_cast<int64_t>(m) * a.ldo + f) = make_uint4(c[0], c[1], c[2], c[3]);
+        if (wn == 0 && g == 0) a.out_scale[static_cast<int64_t>(m) * a.ldos + bn] = static_cast<uint8_t>(ex);
+      }
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -196,7 +593,32 @@ hipError_t launch_gemm_fp8(const GemmFp8Args& a, int epilogue, hipStream_t s) {
     else
       gemm_fp8_kernel<MT, kEpi8Bf16><<<grid, dim3(256), 0, s>>>(a);
   };
-  if (a.M <= 16 * a.E)
+  const bool swiglu = epilogue == kEpi8SwiGLU;
+  auto tiled = [&](auto shape) {
+    using S = decltype(shape);
+    const int blocks = row_blocks(a, S::BM) * ((a.N + S::BN - 1) / S::BN);
+    if constexpr (S::BN == 256) {
+      if (swiglu) {
+        gemm_fp8_tiled_kernel<S, kEpi8SwiGLU><<<dim3(blocks), dim3(256), 0, s>>>(a);
+        return;
+      }
+    }
+    gemm_fp8_tiled_kernel<S, kEpi8Bf16><<<dim3(blocks), dim3(256), 0, s>>>(a);
+  };
+  // The tiled kernel reaches rows by 32-bit byte offsets from its block's first
+  // element, or from the first row of X where rows are gathered.
+  constexpr int64_t kMax = int64_t{1} << 32;
+  const bool fits = static_cast<int64_t>(a.src ? a.x_rows : 256) * a.ldx <= kMax && 256ll * a.Kp <= kMax &&
+                    static_cast<int64_t>(a.N) * (a.Kp / kGroup + 3) <= kMax;
+  if (!fits)
+    go(std::integral_constant<int, 4>{});
+  else if (a.M > 128 * a.E)
+    tiled(TileShape8<8, 8>{});
+  else if (a.M > 64 * a.E)
+    tiled(TileShape8<8, 4>{});
+  else if (a.M > 32 * a.E)
+    tiled(TileShape8<8, 2>{});
+  else if (a.M <= 16 * a.E)
     go(std::integral_constant<int, 1>{});
   else
     go(std::integral_constant<int, 4>{});
