@@ -226,6 +226,17 @@ metro_status metro_op_gemm_fp8(const uint8_t* X, int32_t ldx, const uint8_t* x_s
                                uint16_t* out_bf16, uint8_t* out_fp8, int32_t ldo, uint8_t* out_scale, int32_t ldos,
                                float* workspace, int64_t workspace_bytes, void* stream);
 
+/* What metro_op_gemm_fp8 (n_experts 0) or metro_op_gemm_fp8_experts (M slots; X
+ * gathered or not, its rows within 4 GiB) would run, for inspection and tests;
+ * host only, no device work.  *kind: 0 direct (rows too far apart for the
+ * others' 32-bit offsets; never the answer here), 1 streaming, 2 tiled.  *w_rows,
+ * *x_rows: rows of W and of X of a workgroup.  *k_slices: slices that a finishing
+ * launch sums, 0: none.  Errors: E_INVAL (shape rules of metro_op_gemm_fp8,
+ * NULL outputs). */
+metro_status metro_op_gemm_fp8_plan(int32_t M, int32_t N, int32_t Kp, int32_t epilogue, int32_t n_experts,
+                                    int64_t workspace_bytes, int32_t* kind, int32_t* w_rows, int32_t* x_rows,
+                                    int32_t* k_slices);
+
 /* Routing of T tokens to top_k of n_experts experts each.  With z = logits[t, :]
  * and, in fp64, s = softmax(z) (scoring 0) or 1 / (1 + exp(-z)) (scoring 1):
  *   choice c = s + bias (bias fp32 [n_experts] or NULL; -inf shuts an expert out)

@@ -13,6 +13,7 @@
 // 2^-13 of it: 1.5e-5 of the result's 2-norm on normal data (2.6e-5 where X is
 // a product of normals), against 1.7e-3 that the rounding to bf16 adds behind it.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 #include <utility>
 
@@ -22,6 +23,8 @@
 namespace metro {
 
 namespace {
+
+constexpr int kSlices = 3;  // epilogue of a k slice: its fp32 sums
 
 __device__ __forceinline__ f32x4 mfma8(uint4 a0, uint4 a1, uint4 b0, uint4 b1, f32x4 c, int sa, int sb) {
   const i32x8 a = {static_cast<int>(a0.x), static_cast<int>(a0.y), static_cast<int>(a0.z), static_cast<int>(a0.w),
@@ -103,24 +106,26 @@ __device__ __forceinline__ int64_t source_row(const GemmFp8Args& a, int m) {
 // chunks: the W rows of one half (of both wave rows), and half the X rows of a
 // stage.  During half h = 2 s + p the wave multiplies from registers, reads the W
 // fragments of half h + 1 and half of the X fragments of stage s + 1 (chunk h + 2),
-// and requests chunk h + 5 of both, into slots whose last reads lie behind the
-// previous barrier (W ring 5 chunks, X ring 4).  The barrier that ends the half
-// stands for: W chunk h + 2 and X chunk h + 3 have landed, and what this half read
-// is in registers.  Every memory instruction rides behind a matrix instruction.
-// Scales: four stages' bytes of a row are one word; they have a ring of their
-// own of two groups of four stages, requested four stages ahead.
+// and requests chunk h + D of both, into slots whose last reads lie behind the
+// previous barrier (W ring of D chunks, X ring of D - 1).  The barrier that ends
+// the half stands for: W chunk h + 2 and X chunk h + 3 have landed, and what this
+// half read is in registers.  Every memory instruction rides behind a matrix
+// instruction.  Scales: four stages' bytes of a row are one word; they have a ring
+// of their own of two groups of four stages, requested four stages ahead.
 // ---------------------------------------------------------------------------
-template <int TN_, int TM_>
+template <int TN_, int TM_, int D_ = 5>
 struct TileShape8 {
-  static constexpr int TN = TN_, TM = TM_;
+  static constexpr int TN = TN_, TM = TM_, D = D_;
   static constexpr int BN = 32 * TN, BM = 32 * TM;
-  static constexpr int WR = 5, XR = 4;
+  static constexpr int WR = D, XR = D - 1;
   static constexpr int kW = TN * 2048, kX = TM * 2048;  // bytes of a chunk
   static constexpr int LW = TN / 2, LX = TM / 2;        // wave loads of a chunk, per wave
+  static constexpr int kYoung = (D - 2) * LW + (D - 3) * LX;  // loads that may be under way at a barrier
   static constexpr int kScales = 4 * (BN + BM);         // bytes of a group of four stages
   static constexpr int kLds = WR * kW + XR * kX + 2 * kScales;
   static constexpr int OCC = kLds <= 80 * 1024 ? 2 : 1;
   static_assert(TN % 4 == 0 && TM % 2 == 0, "halves and fragments are shared evenly");
+  static_assert(D >= 4 && kYoung < 63 && kLds <= 160 * 1024, "the ring's loads can be counted and held");
 };
 
 // c += a . b scaled by 2^(sa - 127 + sb - 127) (lowest bytes), the accumulator in
@@ -133,17 +138,23 @@ __device__ __forceinline__ void mfma8_acc(f32x4& c, i32x8 a, i32x8 b, int sa, in
                : "v"(a), "v"(b), "v"(sa), "v"(sb));
 }
 // The same with a direct load of 16 bytes per lane into LDS bytes lds_base + INC +
-// 16 * lane behind it; the matrix instruction is the wait state between the M0
-// write and the load.
-template <int INC>
+// 16 * lane behind it (NT: of data that nobody reads again soon); the matrix
+// instruction is the wait state between the M0 write and the load.
+template <int INC, bool NT>
 __device__ __forceinline__ void mfma8_acc_load(f32x4& c, i32x8 a, i32x8 b, int sa, int sb, const void* base,
                                                uint32_t off, uint32_t lds_base) {
-  asm volatile(
-      "s_add_u32 m0, %5, %6\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]\n\t"
-      "global_load_lds_dwordx4 %7, %8"
-      : "+a"(c)
-      : "v"(a), "v"(b), "v"(sa), "v"(sb), "s"(lds_base), "n"(INC), "v"(off), "s"(base)
-      : "memory", "m0", "scc");
+#define METRO_MFMA8_LOAD(HINT)                                                                                      \
+  asm volatile(                                                                                                     \
+      "s_add_u32 m0, %5, %6\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]\n\t"       \
+      "global_load_lds_dwordx4 %7, %8" HINT                                                                         \
+      : "+a"(c)                                                                                                     \
+      : "v"(a), "v"(b), "v"(sa), "v"(sb), "s"(lds_base), "n"(INC), "v"(off), "s"(base)                               \
+      : "memory", "m0", "scc")
+  if constexpr (NT)
+    METRO_MFMA8_LOAD(" nt");
+  else
+    METRO_MFMA8_LOAD("");
+#undef METRO_MFMA8_LOAD
 }
 // 4 bytes per lane into LDS bytes lds_base + 4 * lane
 __device__ __forceinline__ void lds_load4s(const void* base, uint32_t off, uint32_t lds_base) {
@@ -194,15 +205,30 @@ __device__ __forceinline__ void transpose4(uint32_t (&v)[4]) {
   }
 }
 
-template <class S, int EPI>
-__global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args a) {
+// k slice y of ks: whole groups of four 128-column blocks
+struct KSpan {
+  int first, blocks;
+};
+__device__ __forceinline__ KSpan k_span(int nk, int ks, int y) {
+  const int units = (nk + 3) / 4, lo = units * y / ks * 4, hi = units * (y + 1) / ks * 4;
+  return {lo, min(hi, nk) - lo};
+}
+
+// EPI: kEpi8Bf16, kEpi8SwiGLU or kSlices: the grid's ks k slices leave their
+// fp32 sums in ws[slice][m][n] for gemm_fp8_finish_kernel.  NT: W passes the
+// caches by (plan_gemm_fp8 says when).
+template <class S, int EPI, bool NT>
+__global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args a, int ks) {
   constexpr int TN = S::TN, TM = S::TM, HN = TN / 2, HM = TM / 2, LW = S::LW, LX = S::LX;
   __shared__ uint4 lds[S::kLds / 16];
   const int nb = (a.N + S::BN - 1) / S::BN;
   const int mb = total_row_blocks(a, S::BM);
-  if (static_cast<int>(blockIdx.x) >= mb * nb) return;
+  const int items = mb * nb * ks;
+  if (static_cast<int>(blockIdx.x) >= items) return;
   int bm, bn, e, m0, m1;
-  tile_at<4>(xcd_run(blockIdx.x, mb * nb), mb, nb, bm, bn);
+  const int item = xcd_run(blockIdx.x, items);
+  const int slice = item / (mb * nb);
+  tile_at<4>(item % (mb * nb), mb, nb, bm, bn);
   if (!row_block(a, bm, S::BM, e, m0, m1)) return;
   e = __builtin_amdgcn_readfirstlane(e);
   m0 = __builtin_amdgcn_readfirstlane(m0);
@@ -212,16 +238,18 @@ __global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wn = wave >> 1, wm = wave & 1;
   const int r16 = lane & 15, g = lane >> 4;
-  const int nk = a.Kp / kGroup, groups = padded_groups(a.Kp);
+  const int groups = padded_groups(a.Kp);
+  const KSpan span = k_span(a.Kp / kGroup, ks, slice);
+  const int nk = span.blocks;
 
   // Loads of a chunk: W chunk p of a stage has tiles wn' * HN + i of wave row wn',
   // two KiB halves each; X chunk p has rows 16 (wm' TM + p HM) .. of wave column
   // wm', in blocks of 8.  Tiles and rows past the ends re-read the last ones,
   // whose products only reach outputs that are not stored.
   const char* const wbase = reinterpret_cast<const char*>(a.W) + static_cast<int64_t>(e) * a.N * a.Kp +
-                            static_cast<int64_t>(n0) * a.Kp;
+                            static_cast<int64_t>(n0) * a.Kp + span.first * 2048;
   const int64_t xrow0 = a.src ? 0 : m0;
-  const char* const xbase = reinterpret_cast<const char*>(a.X) + xrow0 * a.ldx;
+  const char* const xbase = reinterpret_cast<const char*>(a.X) + xrow0 * a.ldx + span.first * kGroup;
   uint32_t woff[2][LW], xoff[2][LX];
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
@@ -244,14 +272,15 @@ __global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args
   constexpr uint32_t kXAt = S::WR * S::kW, kSAt = kXAt + S::XR * S::kX;
   const uint32_t wdst = lds0 + wave * LW * 1024, xdst = lds0 + kXAt + wave * LX * 1024;
   // scales: a wave loads words of 64 W rows and of 64 X rows of a group
-  const char* const wsbase = reinterpret_cast<const char*>(a.w_scale) + static_cast<int64_t>(e) * a.N * groups;
-  const char* const xsbase = reinterpret_cast<const char*>(a.x_scale) + xrow0 * a.ldxs;
+  const char* const wsbase = reinterpret_cast<const char*>(a.w_scale) + static_cast<int64_t>(e) * a.N * groups +
+                             span.first * 16;
+  const char* const xsbase = reinterpret_cast<const char*>(a.x_scale) + xrow0 * a.ldxs + span.first;
   const int ws64 = wave % (S::BN / 64), xs64 = wave % (S::BM / 64);
   const uint32_t wsoff = static_cast<uint32_t>(min(n0 / 16 + ws64 * 4 + g, a.N / 16 - 1)) * (groups * 16) + r16 * 4;
   const uint32_t xsoff = static_cast<uint32_t>(source_row(a, min(m0 + xs64 * 64 + lane, m1 - 1)) - xrow0) *
                          static_cast<uint32_t>(a.ldxs);
   auto load_scales = [&](int q) __attribute__((always_inline)) {  // group q (at most the last)
-    const int at = min(q, groups / 4 - 1);
+    const int at = min(q, (nk + 3) / 4 - 1);
     const uint32_t slot = lds0 + kSAt + (q & 1) * S::kScales;
     lds_load4s(wsbase + at * 64, wsoff, slot + ws64 * 256);
     lds_load4s(xsbase + at * 4, xsoff, slot + S::BN * 4 + xs64 * 256);
@@ -305,11 +334,12 @@ __global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args
   load_x(1);
   load_w(0);
   load_w(1);
-  load_x(2);
-  load_w(2);
-  load_x(3);
-  load_w(3);
-  wait_vmcnt<3 * LW + 2 * LX>();
+#pragma unroll
+  for (int c = 2; c < S::D - 1; ++c) {
+    load_x(c);
+    load_w(c);
+  }
+  wait_vmcnt<S::kYoung>();
   lds_barrier();
 #pragma unroll
   for (int u = 0; u < TN; ++u) read_a(fa[0], u, 0);
@@ -319,9 +349,9 @@ __global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args
     for (int h = 0; h < 2; ++h) read_b(fb[0][j], h, j % HM, (j / HM) * S::kX);
   read_scales(0);
   drained_barrier();
-  load_x(4);
-  load_w(4);
-  wait_vmcnt<3 * LW + 2 * LX>();
+  load_x(S::D - 1);
+  load_w(S::D - 1);
+  wait_vmcnt<S::kYoung>();
   drained_barrier();
 
   // One half: P parity of the stage, H half; its W fragments are fa[H].  wo, xo:
@@ -340,12 +370,12 @@ __global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args
          constexpr bool takes = kSlots == NM || U % 2 == 1;
          constexpr int l = takes && first_of(slot, kSlots, ND) < first_of(slot + 1, kSlots, ND) ? first_of(slot, kSlots, ND) : ND;
          f32x4& c = acc[H * HN + i][j];
-         // chunks h + 5: the other half's
+         // chunks h + D
          if constexpr (l < LX)
-           mfma8_acc_load<l * 1024>(c, fa[H][i].all, fb[P][j].all, sw[H * HN + i], sx[j], xsrc, xoff[H ^ 1][l], xd);
+           mfma8_acc_load<l * 1024, false>(c, fa[H][i].all, fb[P][j].all, sw[H * HN + i], sx[j], xsrc, xoff[(H + S::D) & 1][l], xd);
          else if constexpr (l < ND)
-           mfma8_acc_load<(l - LX) * 1024>(c, fa[H][i].all, fb[P][j].all, sw[H * HN + i], sx[j], wsrc,
-                                           woff[H ^ 1][l - LX], wd);
+           mfma8_acc_load<(l - LX) * 1024, NT>(c, fa[H][i].all, fb[P][j].all, sw[H * HN + i], sx[j], wsrc,
+                                           woff[(H + S::D) & 1][l - LX], wd);
          else
            mfma8_acc(c, fa[H][i].all, fb[P][j].all, sw[H * HN + i], sx[j]);
 #pragma unroll
@@ -359,10 +389,10 @@ __global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args
        }()),
        ...);
     }(std::make_integer_sequence<int, NM>{});
-    wait_vmcnt<3 * LW + 2 * LX>();
+    wait_vmcnt<S::kYoung>();
   };
-  // ring offsets of chunk h + 1 (W) and h + 2 (X) to read; of chunk h + 5: W's slot is that of h, X's that of h + 1
-  uint32_t w_read = S::kW, w_put = 0, x_read = 2 * S::kX, x_put = S::kX;
+  // ring offsets of chunk h + 1 (W) and h + 2 (X) to read; of chunk h + D: W's slot is that of h, X's that of h + 1
+  uint32_t w_read = S::kW, w_put = 0, x_read = 2 * S::kX % (S::XR * S::kX), x_put = S::kX;
   auto turn = [&]() __attribute__((always_inline)) {
     w_put = w_read;
     w_read = w_read + S::kW == S::WR * S::kW ? 0 : w_read + S::kW;
@@ -371,7 +401,7 @@ __global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args
   };
   auto stage = [&](auto par, int s) __attribute__((always_inline)) {
     if ((s & 3) == 0) load_scales((s >> 2) + 1);
-    const int s0 = min(s + 2, nk - 1), s1 = min(s + 3, nk - 1);
+    const int s0 = min(s + S::D / 2, nk - 1), s1 = min(s + (S::D + 1) / 2, nk - 1);
     half(par, std::integral_constant<int, 0>{}, w_read, x_read, wbase + s0 * 2048, wdst + w_put, xbase + s0 * kGroup,
          xdst + x_put);
     turn();
@@ -404,7 +434,19 @@ __global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args
   drained_barrier();
 
   const int mw = m0 + wm * 16 * TM, nw = n0 + wn * 16 * TN;
-  if constexpr (EPI == kEpi8Bf16) {
+  if constexpr (EPI == kSlices) {
+    float* const out = a.ws + static_cast<int64_t>(slice) * a.M * a.N;
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int m = mw + 16 * j + r16;
+#pragma unroll
+      for (int i = 0; i < TN; ++i) {
+        const int n = nw + 16 * i + 4 * g;
+        if (m < m1 && n < a.N) *reinterpret_cast<f32x4*>(out + static_cast<int64_t>(m) * a.N + n) = acc[i][j];
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  } else if constexpr (EPI == kEpi8Bf16) {
     // four tiles' words are transposed over the lane groups, so that a lane has
     // the 16 columns of one tile and four lanes a whole line of a row
 #pragma unroll
@@ -473,18 +515,20 @@ __global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args
 
 // ---------------------------------------------------------------------------
 // 256 rows of W x 16 MT rows of X per workgroup, operands straight from global
-// memory, K whole.  A wave has 64 rows of W; the 128 features of a workgroup's
+// memory through 64-bit addresses, K whole: for rows that lie too far apart for
+// the tiled kernel.  A wave has 64 rows of W; the 128 features of a workgroup's
 // SwiGLU output are one group, whose maximum the four waves find through LDS.
 // ---------------------------------------------------------------------------
 template <int MT, int EPI>
 __global__ __launch_bounds__(256) void gemm_fp8_kernel(GemmFp8Args a) {
+  const int nb = (a.N + 255) / 256, bn = blockIdx.x % nb;
   int e, m0, m1;
-  if (!row_block(a, blockIdx.y, 16 * MT, e, m0, m1)) return;
+  if (!row_block(a, blockIdx.x / nb, 16 * MT, e, m0, m1)) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   const int groups = padded_groups(a.Kp), nkb = a.Kp / kGroup;
   const uint8_t* W = a.W + static_cast<int64_t>(e) * a.N * a.Kp;
   const uint8_t* ws = a.w_scale + static_cast<int64_t>(e) * a.N * groups;
-  const int n0 = blockIdx.x * 256 + wave * 64;
+  const int n0 = bn * 256 + wave * 64;
   const uint8_t *wp[4], *wsp[4], *xp[MT], *xsp[MT];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -569,7 +613,146 @@ __global__ __launch_bounds__(256) void gemm_fp8_kernel(GemmFp8Args a) {
           *reinterpret_cast<uint32_t*>(a.out8 + static_cast<int64_t>(m) * a.ldo + f) =
               pack_e4m3(y[p][j][0] * s, y[p][j][1] * s, y[p][j][2] * s, y[p][j][3] * s);
       }
-      if (wave == 0 && g == 0) a.out_scale[static_cast<int64_t>(m) * a.ldos + blockIdx.x] = static_cast<uint8_t>(ex);
+      if (wave == 0 && g == 0) a.out_scale[static_cast<int64_t>(m) * a.ldos + bn] = static_cast<uint8_t>(ex);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Streaming kernel for few rows (16 MT): the weights' bytes are the cost.  A
+// workgroup of NW waves owns 16 NT rows of W; the waves take the slice's groups
+// of four 128-column blocks in turn, each group 8 KiB a row tile of contiguous
+// loads, straight into registers and all in flight at once, and one word of
+// powers for each row.  The waves' sums meet in LDS, in wave order.
+// ---------------------------------------------------------------------------
+template <int MT, int NT, int NW, int EPI>
+__global__ __launch_bounds__(NW * 64) void gemm_fp8_stream_kernel(GemmFp8Args a, int ks) {
+  static_assert(EPI == kEpi8Bf16 || EPI == kSlices, "a group of SwiGLU features spans workgroups");
+  const int nb = (a.N + 16 * NT - 1) / (16 * NT);
+  const int mb = total_row_blocks(a, 16 * MT);
+  const int items = mb * nb * ks;
+  if (static_cast<int>(blockIdx.x) >= items) return;
+  const int item = xcd_run(blockIdx.x, items);
+  const int slice = item / (mb * nb), bn = item % (mb * nb) / mb;
+  int e, m0, m1;
+  if (!row_block(a, item % mb, 16 * MT, e, m0, m1)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int r = lane & 15, g = lane >> 4;
+  const int groups = padded_groups(a.Kp), n0 = bn * 16 * NT;
+  const KSpan span = k_span(a.Kp / kGroup, ks, slice);
+  const uint8_t *wp[NT], *wsp[NT], *xp[MT], *xsp[MT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int64_t tn = min(n0 / 16 + i, a.N / 16 - 1) + static_cast<int64_t>(e) * (a.N / 16);
+    wp[i] = a.W + tn * a.Kp * 16 + static_cast<int64_t>(span.first) * 2048 + lane * 16;
+    wsp[i] = a.w_scale + tn * groups * 16 + span.first * 16 + r * 4;
+  }
+#pragma unroll
+  for (int j = 0; j < MT; ++j) {
+    const int64_t row = source_row(a, min(m0 + 16 * j + r, m1 - 1));
+    xp[j] = a.X + row * a.ldx + static_cast<int64_t>(span.first) * kGroup + 16 * g;
+    xsp[j] = a.x_scale + row * a.ldxs + span.first;
+  }
+  f32x4 acc[NT][MT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int u = wave; 4 * u < span.blocks; u += NW) {
+    uint4 w[4][NT][2], x[4][MT][2];
+    int sw[NT], sx[MT];
+    // (blocks behind the slice's last re-read it and are not multiplied)
+#pragma unroll
+    for (int i = 0; i < NT; ++i) sw[i] = *reinterpret_cast<const int*>(wsp[i] + u * 64);
+#pragma unroll
+    for (int j = 0; j < MT; ++j) sx[j] = *reinterpret_cast<const int*>(xsp[j] + u * 4);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t kb = min(4 * u + q, span.blocks - 1);
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) w[q][i][h] = *reinterpret_cast<const uint4*>(wp[i] + kb * 2048 + h * 1024);
+#pragma unroll
+      for (int j = 0; j < MT; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) x[q][j][h] = *reinterpret_cast<const uint4*>(xp[j] + kb * kGroup + h * 64);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (4 * u + q >= span.blocks) break;
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+          acc[i][j] = mfma8(w[q][i][0], w[q][i][1], x[q][j][0], x[q][j][1], acc[i][j], sw[i] >> (8 * q), sx[j] >> (8 * q));
+    }
+  }
+  __shared__ f32x4 red[NW][NT * MT][kWave];
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) red[wave][i * MT + j][lane] = acc[i][j];
+  __syncthreads();
+  for (int t = wave; t < NT * MT; t += NW) {
+    f32x4 sum = red[0][t][lane];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) sum += red[w][t][lane];
+    const int m = m0 + 16 * (t % MT) + r, n = n0 + 16 * (t / MT) + 4 * g;
+    if (m >= m1 || n >= a.N) continue;
+    if constexpr (EPI == kSlices)
+      *reinterpret_cast<f32x4*>(a.ws + (static_cast<int64_t>(slice) * a.M + m) * a.N + n) = sum;
+    else
+      *reinterpret_cast<uint2*>(a.out16 + static_cast<int64_t>(m) * a.ldo + n) =
+          make_uint2(pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3]));
+  }
+}
+
+// Sum of ks slices in slice order, and the epilogue: bf16 rows (a thread 4
+// columns), or SwiGLU to 8-bit rows (32 lanes a group of 128 features, 4 each).
+// By experts, rows that no expert has are left alone.
+template <int EPI>
+__global__ __launch_bounds__(256) void gemm_fp8_finish_kernel(GemmFp8Args a, int ks) {
+  constexpr bool kGate = EPI == kEpi8SwiGLU;
+  const int per_row = kGate ? (a.N / 2 + kGroup - 1) / kGroup * 32 : a.N / 4;
+  const int64_t n = static_cast<int64_t>(a.M) * per_row, slice = static_cast<int64_t>(a.M) * a.N;
+  int lo = 0, hi = a.M;
+  if (a.offsets) {
+    lo = a.offsets[0];
+    hi = a.offsets[a.E];
+  }
+  for (int64_t u = blockIdx.x * 256ll + threadIdx.x; u < n; u += 256ll * gridDim.x) {
+    const int m = static_cast<int>(u / per_row), c = static_cast<int>(u % per_row) * 4;
+    if (m < lo || m >= hi) continue;  // (whole groups of lanes)
+    auto sum = [&](int col) {
+      const float* p = a.ws + static_cast<int64_t>(m) * a.N + col;
+      f32x4 v = *reinterpret_cast<const f32x4*>(p);
+      for (int k = 1; k < ks; ++k) v += *reinterpret_cast<const f32x4*>(p + k * slice);
+      return v;
+    };
+    if constexpr (kGate) {
+      const int col = 16 * (c / 8) + c % 8;  // gate column of feature c
+      f32x4 y = {0.f, 0.f, 0.f, 0.f};
+      float best = 0.f;
+      if (col < a.N) {
+        const f32x4 gate = sum(col), up = sum(col + 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          y[i] = silu_f32(gate[i]) * up[i];
+          best = fmaxf(best, fabsf(y[i]));
+        }
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor(best, o, 32));
+      const int ex = e8m0_of(best);
+      const float s = e8m0_inverse(ex);
+      *reinterpret_cast<uint32_t*>(a.out8 + static_cast<int64_t>(m) * a.ldo + c) =
+          pack_e4m3(y[0] * s, y[1] * s, y[2] * s, y[3] * s);
+      if (c % kGroup == 0) a.out_scale[static_cast<int64_t>(m) * a.ldos + c / kGroup] = static_cast<uint8_t>(ex);
+    } else {
+      const f32x4 v = sum(c);
+      *reinterpret_cast<uint2*>(a.out16 + static_cast<int64_t>(m) * a.ldo + c) =
+          make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
     }
   }
 }
@@ -581,48 +764,165 @@ int row_blocks(const GemmFp8Args& a, int BM) {
   return static_cast<int>(std::min<int64_t>(a.M, (a.M + static_cast<int64_t>(a.E) * (BM - 1)) / BM));
 }
 
+// go with the smallest number of LO, LO + STEP .. HI that is at least v (HI if none)
+template <int LO, int STEP, int HI, class Go>
+void one_of(int v, Go&& go) {
+  if constexpr (LO < HI) {
+    if (v > LO) return one_of<LO + STEP, STEP, HI>(v, go);
+  }
+  go(std::integral_constant<int, LO>{});
+}
+
+// Row blocks to expect of M rows; by experts, half a partly filled one each on
+// top, and at least one for each expert.
+double expected_blocks(const GemmFp8Args& a, int BM) {
+  if (!a.offsets) return (a.M + BM - 1) / BM;
+  const int live = std::min(a.E, a.M);
+  return std::max<double>(live, static_cast<double>(a.M) / BM + 0.5 * live);
+}
+
+// us that a plan is expected to take: the launch, the larger of the rounds of
+// workgroups and the stream of the weights, and what k slices cost behind it.
+double expected_us(const GemmFp8Args& a, int epilogue, const GemmFp8Plan& p) {
+  constexpr double kLaunch = 3.0;
+  const int ks = std::max(p.ks, 1), stages = (a.Kp / kGroup + ks - 1) / ks;
+  const int live = a.offsets ? std::min(a.E, a.M) : 1;  // matrices that have rows
+  const double finish = p.ks ? 2.6 + 8e-6 * ks * a.M * a.N / 5.0 : 0.0;
+  const int bm = 16 * p.mt * (p.kind == GemmFp8Kind::kTiled ? 2 : 1), bn = p.kind == GemmFp8Kind::kTiled ? 32 * p.nt : 32;
+  const double blocks = expected_blocks(a, bm) * ((a.N + bn - 1) / bn) * ks;
+  // MB; row blocks that read the same weights share them in the caches in part
+  const double weights = 1e-6 * a.N * a.Kp * (live + 0.6 * (expected_blocks(a, bm) - live));
+  if (p.kind == GemmFp8Kind::kStream) return kLaunch + weights / std::min(p.mt == 1 ? 5.2 : 4.0, 0.02 * blocks) + finish;
+  constexpr int kCus = 256;
+  // (how the rows of experts fall into rounds is not known)
+  double rounds = a.offsets ? std::max(1.0, blocks / kCus + 0.5) : std::ceil(blocks / kCus);
+  if (rounds > 1 && p.nt == 4 && p.mt <= 4) rounds *= 0.85;  // two workgroups share a CU
+  const double stage = 0.25 + 0.018 * p.nt * p.mt;
+  const double gate = epilogue == kEpi8SwiGLU && !p.ks ? 0.5 * p.mt : 0.0;
+  const double c = rounds * (stages * stage + gate), h = weights / std::min(5.6, 0.03 * blocks);
+  return kLaunch + std::sqrt(std::sqrt(c * c * c * c + h * h * h * h)) + finish;  // (overlapped, not freely)
+}
+
+// Whether W should pass the caches by.  It gains where W streams from HBM and few
+// row blocks read each matrix, more so by experts, whose row blocks of one
+// matrix are neighbours in time (W kept / passed, us): 8B gate/up at 128 / 301 /
+// 1001 rows 33.0 / 29.9, 45.0 / 43.3, 106.7 / 104.1, at 4096 377 / 388; 70B down at 128
+// rows 55.2 / 54.0, at 301 (two row blocks) 87.0 / 90.5; QKV of 4096 x 4096 at 301
+// rows, kept between calls, 14.3 / 17.8; eight experts' gate/up of 50 rows 168.9 /
+// 156.5, of 2000 362 / 355, their down of 50 80.5 / 70.6, of 8192 448 / 426.
+bool passes_caches(const GemmFp8Args& a, const GemmFp8Plan& p) {
+  const int live = a.offsets ? std::min(a.E, a.M) : 1;
+  const double per = expected_blocks(a, 32 * p.mt) / live;
+  return 1e-6 * a.N * a.Kp * live >= 64 && per <= (a.offsets ? 6 : a.N >= 16384 ? 4 : 1);
+}
+
 }  // namespace
 
-hipError_t launch_gemm_fp8(const GemmFp8Args& a, int epilogue, hipStream_t s) {
-  if (a.M <= 0) return hipSuccess;
-  auto go = [&](auto mt) {
-    constexpr int MT = decltype(mt)::value;
-    const dim3 grid((a.N + 255) / 256, row_blocks(a, 16 * MT));
-    if (epilogue == kEpi8SwiGLU)
-      gemm_fp8_kernel<MT, kEpi8SwiGLU><<<grid, dim3(256), 0, s>>>(a);
-    else
-      gemm_fp8_kernel<MT, kEpi8Bf16><<<grid, dim3(256), 0, s>>>(a);
-  };
-  const bool swiglu = epilogue == kEpi8SwiGLU;
-  auto tiled = [&](auto shape) {
-    using S = decltype(shape);
-    const int blocks = row_blocks(a, S::BM) * ((a.N + S::BN - 1) / S::BN);
-    if constexpr (S::BN == 256) {
-      if (swiglu) {
-        gemm_fp8_tiled_kernel<S, kEpi8SwiGLU><<<dim3(blocks), dim3(256), 0, s>>>(a);
-        return;
-      }
-    }
-    gemm_fp8_tiled_kernel<S, kEpi8Bf16><<<dim3(blocks), dim3(256), 0, s>>>(a);
-  };
+// Kernel and k slices: of the plans that the shape and the workspace allow, the
+// one with the least expected time.  What the expectation knows was measured with
+// weights out of the caches, us:
+//  - a tiled stage (128 columns) takes about 0.25 + 0.018 TN TM of a CU, LDS and
+//    barriers first, the matrix cores from TN TM = 48 on: 16 x 32 row tiles (TN, TM)
+//    = 4, 2 0.42; 4, 4 0.54; 4, 8 0.77; 8, 2 0.55; 8, 4 0.79; 8, 6 1.1; 8, 8 1.4.  So
+//    rows are not rounded up to large tiles (8B gate/up at 301 rows as 256 x 256 /
+//    256 x 192 / 256 x 128 tiles 53.6 / 43.2 / 59.6, at 200 rows 48.5 / 43.8 / 37.4),
+//    and rounds of 256 workgroups count whole (8192 rows of 8 experts' down as 256 x
+//    256 / 256 x 192 477 / 449).
+//  - weights stream at 5.6 TB/s where enough workgroups ask: 8B gate/up at 25 rows as
+//    112 workgroups of 256 W rows with SwiGLU in place 31.4, as 224 of 128 with the
+//    finishing launch 25.8.
+//    Further row blocks of the same weights cost about half of it each: 70B down at
+//    128 rows as 2 x 64 rows in 2 slices 70.2, as 128 in 4 55.6; eight experts' gate/up
+//    of 2000 rows in blocks of 128 / 256 361 / 291.
+//  - k slices fill the CUs of narrow products and cost a launch and their sums'
+//    traffic: 70B down at 128 rows in 1 / 2 / 4 / 8 slices of 128 x 128 tiles 121 / 72 /
+//    55.6 / 64, QKV at 301 rows in 1 / 2 16.4 / 21.3.
+//  - up to 32 rows (of each expert) the streaming kernel keeps a narrow product of
+//    few bytes in flight at once: QKV at 25 rows 8.4 against 10.9 of 4 tiled slices,
+//    8B down at 16 rows 15.9 / 17.8, but 70B QKV at 32 rows 26.9 / 23.6.
+GemmFp8Plan plan_gemm_fp8(const GemmFp8Args& a, int epilogue) {
   // The tiled kernel reaches rows by 32-bit byte offsets from its block's first
   // element, or from the first row of X where rows are gathered.
   constexpr int64_t kMax = int64_t{1} << 32;
   const bool fits = static_cast<int64_t>(a.src ? a.x_rows : 256) * a.ldx <= kMax && 256ll * a.Kp <= kMax &&
                     static_cast<int64_t>(a.N) * (a.Kp / kGroup + 3) <= kMax;
-  if (!fits)
-    go(std::integral_constant<int, 4>{});
-  else if (a.M > 128 * a.E)
-    tiled(TileShape8<8, 8>{});
-  else if (a.M > 64 * a.E)
-    tiled(TileShape8<8, 4>{});
-  else if (a.M > 32 * a.E)
-    tiled(TileShape8<8, 2>{});
-  else if (a.M <= 16 * a.E)
-    go(std::integral_constant<int, 1>{});
+  if (!fits) return {GemmFp8Kind::kDirect, 16, 4, 0, false};
+  const bool swiglu = epilogue == kEpi8SwiGLU;
+  const int units = (a.Kp / kGroup + 3) / 4;
+  GemmFp8Plan best{GemmFp8Kind::kTiled, 8, 2, 0, false};
+  double least = expected_us(a, epilogue, best);
+  auto offer = [&](GemmFp8Plan p) {
+    if (p.ks > units || static_cast<int64_t>(p.ks) * a.M * a.N > a.ws_floats) return;
+    const double t = expected_us(a, epilogue, p);
+    if (t < least) {
+      least = t;
+      best = p;
+    }
+  };
+  for (int ks = 0; ks <= 8; ks = ks ? 2 * ks : 1) {
+    if (ks == 1 && !swiglu) continue;  // (a product in one slice needs no finishing launch)
+    for (int mt = 2; mt <= 8; mt += 2) {
+      if (ks || !swiglu) offer({GemmFp8Kind::kTiled, 4, mt, ks, false});
+      if (ks != 1) offer({GemmFp8Kind::kTiled, 8, mt, ks, false});
+    }
+    if (a.M <= 32 * (a.offsets ? a.E : 1) && (ks || !swiglu)) offer({GemmFp8Kind::kStream, 2, a.M <= 16 * a.E ? 1 : 2, ks, false});
+  }
+  best.nt_hint = best.kind == GemmFp8Kind::kTiled && passes_caches(a, best);
+  return best;
+}
+
+static hipError_t run_plan(const GemmFp8Plan& p, const GemmFp8Args& a, int epilogue, hipStream_t s) {
+  const int ks = std::max(p.ks, 1);
+  auto grid = [&](int bm, int bn) {
+    return dim3(static_cast<uint32_t>(static_cast<int64_t>(row_blocks(a, bm)) * ((a.N + bn - 1) / bn) * ks));
+  };
+  if (p.kind == GemmFp8Kind::kDirect) {
+    if (epilogue == kEpi8SwiGLU)
+      gemm_fp8_kernel<4, kEpi8SwiGLU><<<grid(64, 256), dim3(256), 0, s>>>(a);
+    else
+      gemm_fp8_kernel<4, kEpi8Bf16><<<grid(64, 256), dim3(256), 0, s>>>(a);
+  } else if (p.kind == GemmFp8Kind::kStream) {
+    one_of<1, 1, 2>(p.mt, [&](auto mt) {
+      if (p.ks)
+        gemm_fp8_stream_kernel<mt, 2, 8, kSlices><<<grid(16 * mt, 32), dim3(512), 0, s>>>(a, ks);
+      else
+        gemm_fp8_stream_kernel<mt, 2, 8, kEpi8Bf16><<<grid(16 * mt, 32), dim3(512), 0, s>>>(a, ks);
+    });
+  } else {
+    one_of<4, 4, 8>(p.nt, [&](auto tn) {
+      one_of<2, 2, 8>(p.mt, [&](auto tm) {
+        using S = TileShape8<tn, tm>;
+        auto go = [&](auto epi, auto nt) {
+          gemm_fp8_tiled_kernel<S, epi, nt><<<grid(S::BM, S::BN), dim3(256), 0, s>>>(a, ks);
+        };
+        auto hinted = [&](auto epi) {
+          if (p.nt_hint)
+            go(epi, std::true_type{});
+          else
+            go(epi, std::false_type{});
+        };
+        if (p.ks) return hinted(std::integral_constant<int, kSlices>{});
+        if constexpr (S::BN == 256) {
+          if (epilogue == kEpi8SwiGLU) return hinted(std::integral_constant<int, kEpi8SwiGLU>{});
+        }
+        hinted(std::integral_constant<int, kEpi8Bf16>{});
+      });
+    });
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.ks) return e;
+  const int64_t items = static_cast<int64_t>(a.M) * (epilogue == kEpi8SwiGLU ? (a.N / 2 + kGroup - 1) / kGroup * 32 : a.N / 4);
+  const dim3 g(static_cast<uint32_t>(std::min<int64_t>((items + 255) / 256, 65536)));
+  if (epilogue == kEpi8SwiGLU)
+    gemm_fp8_finish_kernel<kEpi8SwiGLU><<<g, dim3(256), 0, s>>>(a, ks);
   else
-    go(std::integral_constant<int, 4>{});
+    gemm_fp8_finish_kernel<kEpi8Bf16><<<g, dim3(256), 0, s>>>(a, ks);
   return hipGetLastError();
+}
+
+hipError_t launch_gemm_fp8(const GemmFp8Args& a, int epilogue, hipStream_t s) {
+  if (a.M <= 0) return hipSuccess;
+  return run_plan(plan_gemm_fp8(a, epilogue), a, epilogue, s);
 }
 
 }  // namespace metro

@@ -84,6 +84,15 @@ struct GemmFp8Args {
   int64_t ws_floats;
   int ldx, ldxs, ldo, ldos, Kp, M, N, E, x_rows;
 };
+
+enum class GemmFp8Kind { kDirect, kStream, kTiled };
+struct GemmFp8Plan {
+  GemmFp8Kind kind;
+  int nt, mt;  // 16-row tiles of W and of X: of a workgroup, kTiled: of each of its 2 x 2 waves
+  int ks;      // k slices through the workspace and a finishing launch; 0: none
+  bool nt_hint;  // kTiled: W passes the caches by
+};
+GemmFp8Plan plan_gemm_fp8(const GemmFp8Args& a, int epilogue);
 hipError_t launch_gemm_fp8(const GemmFp8Args& a, int epilogue, hipStream_t s);
 
 }  // namespace metro

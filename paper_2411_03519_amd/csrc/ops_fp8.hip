@@ -89,6 +89,28 @@ metro_status metro_op_gemm_fp8(const uint8_t* X, int32_t ldx, const uint8_t* x_s
   return gemm_fp8("gemm_fp8", a, epilogue, workspace, workspace_bytes, stream);
 }
 
+metro_status metro_op_gemm_fp8_plan(int32_t M, int32_t N, int32_t Kp, int32_t epilogue, int32_t n_experts,
+                                    int64_t workspace_bytes, int32_t* kind, int32_t* w_rows, int32_t* x_rows,
+                                    int32_t* k_slices) {
+  clear_error();
+  if (!kind || !w_rows || !x_rows || !k_slices || M <= 0 || N <= 0 || N % 32 || Kp <= 0 || Kp % 128 || n_experts < 0 ||
+      workspace_bytes < 0 || (epilogue != metro::kEpi8Bf16 && epilogue != metro::kEpi8SwiGLU))
+    return report(METRO_E_INVAL, "gemm_fp8_plan: bad shape (N %% 32, Kp %% 128), epilogue or NULL output");
+  static const int32_t some = 0;
+  metro::GemmFp8Args a{};
+  a.offsets = n_experts ? &some : nullptr;  // (not read)
+  a.E = n_experts ? n_experts : 1;
+  a.M = M, a.N = N, a.Kp = a.ldx = Kp;
+  a.ws_floats = workspace_bytes / 4;
+  const metro::GemmFp8Plan p = metro::plan_gemm_fp8(a, epilogue);
+  const int waves = p.kind == metro::GemmFp8Kind::kTiled ? 2 : 1;
+  *kind = static_cast<int32_t>(p.kind);
+  *w_rows = 16 * p.nt * waves;
+  *x_rows = 16 * p.mt * waves;
+  *k_slices = p.ks;
+  return METRO_OK;
+}
+
 metro_status metro_op_route(const float* logits, int32_t ldl, const float* bias, int32_t T, int32_t n_experts,
                             int32_t scoring, int32_t n_groups, int32_t top_groups, int32_t top_k, int32_t renormalise,
                             float scale, int32_t* experts, float* weights, int32_t* offsets, int32_t* src, int32_t* slot,

@@ -87,6 +87,7 @@ _SIGS = {
                                     _i32, _vp]),
     "metro_op_gemm_fp8": (_i32, [_vp, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _i32, _vp, _i32, _vp,
                                  _i64, _vp]),
+    "metro_op_gemm_fp8_plan": (_i32, [_i32, _i32, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _vp]),
     "metro_op_route": (_i32, [_vp, _i32, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, ctypes.c_float, _vp, _vp, _vp, _vp,
                               _vp, _vp, _i64, _vp]),
     "metro_op_gemm_fp8_experts": (_i32, [_vp, _i32, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32, _vp,
@@ -140,6 +141,10 @@ def _stream(stream) -> int | None:
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
     import torch
+    # the stream's address without a Stream object around it, where torch offers that (2.7 us of a small call)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is not None and torch.cuda.is_initialized():
+        return raw(torch.cuda.current_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -398,6 +403,17 @@ def op_gemm_fp8(X, x_scale, W, w_scale, M: int, N: int, Kp: int, epilogue: int, 
                                 _pad(Kp // 128, 4) if ldxs is None else ldxs, _ptr(W), _ptr(w_scale), Kp, M, N, epilogue,
                                 o16, o8, ldo, _ptr(out_scale), ldos, _ptr(workspace), _bytes(workspace),
                                 _stream(stream)))
+
+
+GEMM_FP8_KINDS = ("direct", "stream", "tiled")
+
+
+def op_gemm_fp8_plan(M: int, N: int, Kp: int, epilogue: int, n_experts: int = 0, workspace_bytes: int = 0):
+    """(kernel kind name, W rows, X rows of a workgroup, k slices) of op_gemm_fp8 (n_experts 0) or
+    op_gemm_fp8_experts; host only."""
+    v = [ctypes.c_int32() for _ in range(4)]
+    check(lib.metro_op_gemm_fp8_plan(M, N, Kp, epilogue, n_experts, workspace_bytes, *[ctypes.byref(x) for x in v]))
+    return GEMM_FP8_KINDS[v[0].value], v[1].value, v[2].value, v[3].value
 
 
 def op_route(logits, T: int, n_experts: int, top_k: int, experts, weights, offsets, src, slot, bias=None,
