@@ -59,10 +59,17 @@ constexpr double kNone = __builtin_nan("");  // an expert that can no longer be 
 // a score to choose by: a NaN comes behind every number
 __device__ __forceinline__ double choosable(double c) { return c == c ? c : -__builtin_inf(); }
 
+// Order of the wave's own LDS accesses (which the hardware keeps) for the compiler.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Scores and choices of the token of this lane's LPT lanes (lane l of them has
-// experts l, l + LPT, ...), t < T valid.  room: LDS of the token, E + 2 * groups
-// doubles (used with groups > 1).  mask: LDS bit sets of the block's tokens, one
-// per expert; bit: the token's.  Every thread of the block calls it.
+// experts l, l + LPT, ...), t < T valid.  room: LDS of the token, E + groups
+// doubles (used with groups > 1, by the token's own lanes only).  mask: LDS bit
+// sets of the block's tokens, one per expert; bit: the token's.  Every lane of
+// the wave calls it.
 template <int LPT, int EPL>
 __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, bool valid, int l, double* room,
                                             unsigned long long* mask, int bit) {
@@ -105,32 +112,43 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, bool 
     c[q] = e < a.E ? choosable(s[q] + (a.bias ? static_cast<double>(a.bias[e]) : 0.0)) : kNone;
   }
   if (a.groups > 1) {
+    // `parts` neighbouring lanes to a group, each with every parts-th expert
     const int per = a.E / a.groups;
-    double *const best = room + a.E, *const kept = best + a.groups;
+    int parts = 1;
+    while (2 * parts * a.groups <= LPT) parts *= 2;
+    const int g = l / parts, part = l % parts;
+    double* const best = room + a.E;
+    wave_fence();
 #pragma unroll
     for (int q = 0; q < EPL; ++q)
       if (q * LPT + l < a.E) room[q * LPT + l] = c[q];
-    __syncthreads();
-    for (int g = l; g < a.groups; g += LPT) {
-      double first = room[g * per], second = -__builtin_inf();
-      for (int i = 1; i < per; ++i) {
+    wave_fence();
+    double first = -__builtin_inf(), second = first;
+    if (g < a.groups)
+      for (int i = part; i < per; i += parts) {
         const double v = room[g * per + i];
         second = fmax(second, fmin(first, v));
         first = fmax(first, v);
       }
-      best[g] = choosable(per > 1 ? first + second : first);
+    for (int o = 1; o < parts; o *= 2) {
+      const double f = __shfl_xor(first, o), h = __shfl_xor(second, o);
+      second = fmax(fmin(first, f), fmax(second, h));
+      first = fmax(first, f);
     }
-    __syncthreads();
-    for (int g = l; g < a.groups; g += LPT) {
-      int ahead = 0;
-      for (int i = 0; i < a.groups; ++i) ahead += best[i] > best[g] || (best[i] == best[g] && i < g);
-      kept[g] = ahead < a.top_groups ? 1.0 : 0.0;
-    }
-    __syncthreads();
+    const double mine = choosable(per > 1 ? first + second : first);
+    if (g < a.groups && part == 0) best[g] = mine;
+    wave_fence();
+    int ahead = 0;
+    if (g < a.groups)
+      for (int i = part; i < a.groups; i += parts) ahead += best[i] > mine || (best[i] == mine && i < g);
+    for (int o = 1; o < parts; o *= 2) ahead += __shfl_xor(ahead, o);
+    wave_fence();
+    if (g < a.groups && part == 0) best[g] = ahead < a.top_groups ? 1.0 : 0.0;
+    wave_fence();
 #pragma unroll
     for (int q = 0; q < EPL; ++q) {
       const int e = q * LPT + l;
-      if (e < a.E && kept[e / per] == 0.0) c[q] = kNone;
+      if (e < a.E && best[e / per] == 0.0) c[q] = kNone;
     }
   }
   const int shift = (threadIdx.x & 63) / LPT * LPT;
@@ -212,7 +230,7 @@ __global__ __launch_bounds__(NTH) void route_kernel(RouteArgs a) {
   const int mine = threadIdx.x / LPT;
   for (int i0 = 0; i0 < n; i0 += kPerPass) {
     const int i = i0 + mine;
-    route_token<LPT, EPL>(a, t0 + i, i < n, threadIdx.x % LPT, room + mine * (a.E + 2 * a.groups), mask, i);
+    route_token<LPT, EPL>(a, t0 + i, i < n, threadIdx.x % LPT, room + mine * (a.E + a.groups), mask, i);
   }
   __syncthreads();
   if (!ALONE) {
@@ -258,16 +276,34 @@ __global__ __launch_bounds__(256) void route_scan_kernel(int32_t* ws, int nb) {
 }
 
 // Places of a block's tokens: the rows of its experts before it, then its own
-// tokens in order.
+// tokens in order.  SCANNED: ws went through route_scan_kernel.
+template <bool SCANNED>
 __global__ __launch_bounds__(256) void route_place_kernel(RouteArgs a, int nb) {
   __shared__ unsigned long long mask[kRouteMaxExperts];
   __shared__ int32_t base[kRouteMaxExperts + 1], wave_sums[4];
   const int b = blockIdx.x;
   const int64_t t0 = static_cast<int64_t>(b) * kRouteBlock;
   const int n = static_cast<int>(min(static_cast<int64_t>(kRouteBlock), a.T - t0));
-  for (int e = threadIdx.x; e < a.E; e += 256) {
+  int before[kRouteMaxExperts / 256];  // rows of the thread's experts in earlier blocks
+#pragma unroll
+  for (int j = 0; j < kRouteMaxExperts / 256; ++j) {
+    const int e = threadIdx.x + 256 * j;
+    if (e >= a.E) break;
+    const int32_t* v = a.ws + static_cast<int64_t>(e) * nb;
+    int here = 0, all = 0;
+    if (SCANNED) {
+      here = b > 0 ? v[b - 1] : 0;
+      all = v[nb - 1];
+    } else {
+      for (int i = 0; i < nb; ++i) {
+        const int n_i = v[i];
+        here += i < b ? n_i : 0;
+        all += n_i;
+      }
+    }
     mask[e] = 0;
-    base[e] = a.ws[static_cast<int64_t>(e) * nb + nb - 1];
+    base[e] = all;
+    before[j] = here;
   }
   __syncthreads();
   prefix<256>(base, a.E, wave_sums);
@@ -275,8 +311,11 @@ __global__ __launch_bounds__(256) void route_place_kernel(RouteArgs a, int nb) {
     for (int e = threadIdx.x; e <= a.E; e += 256) a.offsets[e] = base[e];
   for (int u = threadIdx.x; u < n * a.k; u += 256) atomicOr(&mask[a.experts[t0 * a.k + u]], 1ull << (u / a.k));
   __syncthreads();
-  if (b > 0)
-    for (int e = threadIdx.x; e < a.E; e += 256) base[e] += a.ws[static_cast<int64_t>(e) * nb + b - 1];
+#pragma unroll
+  for (int j = 0; j < kRouteMaxExperts / 256; ++j) {
+    const int e = threadIdx.x + 256 * j;
+    if (e < a.E) base[e] += before[j];
+  }
   __syncthreads();
   for (int u = threadIdx.x; u < n * a.k; u += 256) {
     const int e = a.experts[t0 * a.k + u], i = u / a.k;
@@ -290,41 +329,47 @@ template <int NTH, bool ALONE>
 void launch_choices(const RouteArgs& a, int nb, hipStream_t s) {
   auto go = [&](auto lpt, auto epl) {
     constexpr int LPT = decltype(lpt)::value, EPL = decltype(epl)::value;
-    const uint32_t room = a.groups > 1 ? static_cast<uint32_t>(NTH / LPT * (a.E + 2 * a.groups) * sizeof(double)) : 0;
+    const uint32_t room = a.groups > 1 ? static_cast<uint32_t>(NTH / LPT * (a.E + a.groups) * sizeof(double)) : 0;
     route_kernel<NTH, LPT, EPL, ALONE><<<dim3(nb), dim3(NTH), room, s>>>(a);
   };
   using std::integral_constant;
-  if (a.E <= 8)
-    go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
-  else if (a.E <= 16)
-    go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
-  else if (a.E <= 32)
-    go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
-  else if (a.E <= 64)
-    go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-  else if (a.E <= 128)
-    go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-  else if (a.E <= 256)
-    go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
-  else
-    go(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  constexpr bool kFew = ALONE || NTH == 1024, kMany = NTH == 512;  // up to 256 experts; more
+  if constexpr (kFew) {
+    if (a.E <= 8) return go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+    if (a.E <= 16) return go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+    if (a.E <= 32) return go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+    if (a.E <= 64) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    if (a.E <= 128) return go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    if (a.E <= 256) return go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  }
+  if constexpr (kMany) go(integral_constant<int, 64>{}, integral_constant<int, 8>{});
 }
 
 }  // namespace
 
+// Blocks of kRouteBlock tokens up to which each adds up the counts of all itself.
+constexpr int kRouteOwnSums = 32;
+
 hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
-  if (a.T <= kRouteBlock) {
+  const int nb = (a.T + kRouteBlock - 1) / kRouteBlock;
+  if (nb <= 1) {
     launch_choices<512, true>(a, 1, s);
     return hipGetLastError();
   }
-  const int nb = (a.T + kRouteBlock - 1) / kRouteBlock;
-  launch_choices<256, false>(a, nb, s);
+  if (a.E <= 256)
+    launch_choices<1024, false>(a, nb, s);
+  else
+    launch_choices<512, false>(a, nb, s);  // (room of 512 experts for 16 tokens at a time would pass 64 KiB)
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  if (nb <= kRouteOwnSums) {
+    route_place_kernel<false><<<dim3(nb), dim3(256), 0, s>>>(a, nb);
+    return hipGetLastError();
+  }
   route_scan_kernel<<<dim3(a.E), dim3(256), 0, s>>>(a.ws, nb);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  route_place_kernel<<<dim3(nb), dim3(256), 0, s>>>(a, nb);
+  route_place_kernel<true><<<dim3(nb), dim3(256), 0, s>>>(a, nb);
   return hipGetLastError();
 }
 
