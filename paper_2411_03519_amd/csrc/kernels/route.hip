@@ -54,6 +54,24 @@ __device__ __forceinline__ double lanes_reduce(double v, Op op) {
   return v;
 }
 
+// the largest over the LPT lanes of a token
+template <int LPT>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+  v = max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), 0xB1, 0xf, 0xf, true)));
+  v = max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), 0x4E, 0xf, 0xf, true)));
+  v = max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), 0x141, 0xf, 0xf, true)));
+  if (LPT >= 16) v = max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), 0x140, 0xf, 0xf, true)));
+  if (LPT >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max(r[0], r[1]);
+  }
+  if (LPT >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = max(r[0], r[1]);
+  }
+  return v;
+}
+
 constexpr double kNone = __builtin_nan("");  // an expert that can no longer be chosen
 
 // a score to choose by: a NaN comes behind every number
@@ -69,22 +87,16 @@ __device__ __forceinline__ void wave_fence() {
 // experts l, l + LPT, ...), t < T valid.  room: LDS of the token, E + groups
 // doubles (used with groups > 1, by the token's own lanes only).  mask: LDS bit
 // sets of the block's tokens, one per expert; bit: the token's.  Every lane of
-// the wave calls it.
+// the wave calls it.  z: the logits of its experts, -inf behind the last.
 template <int LPT, int EPL>
-__device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, bool valid, int l, double* room,
-                                            unsigned long long* mask, int bit) {
-  const float* row = a.logits + (valid ? t : 0) * a.ldl;
+__device__ __forceinline__ void route_token(const RouteArgs& a, const float (&z)[EPL], int64_t t, bool valid, int l,
+                                            double* room, unsigned long long* mask, int bit) {
   double s[EPL], c[EPL];
   int place[EPL];
-  float z[EPL];
   auto mx = [](double x, double y) { return fmax(x, y); };
   auto add = [](double x, double y) { return x + y; };
 #pragma unroll
-  for (int q = 0; q < EPL; ++q) {
-    const int e = q * LPT + l;
-    z[q] = e < a.E ? row[e] : -__builtin_inff();
-    place[q] = -1;
-  }
+  for (int q = 0; q < EPL; ++q) place[q] = -1;
   if (a.sigmoid) {
 #pragma unroll
     for (int q = 0; q < EPL; ++q) s[q] = 1.0 / (1.0 + exp(-static_cast<double>(z[q])));
@@ -151,21 +163,49 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, bool 
       if (e < a.E && best[e / per] == 0.0) c[q] = kNone;
     }
   }
-  const int shift = (threadIdx.x & 63) / LPT * LPT;
-  for (int j = 0; j < a.k; ++j) {
-    double m = c[0];
+  // The k largest, one after another.  A choice's upper 32 bits, as an integer of
+  // the same order, mostly tell the largest alone; where two share them (in any
+  // token of the wave) the doubles decide, and their ties the lowest index.
+  // (31527 tokens over 128 experts, 8 chosen: doubles alone 49.5 us, so 41.8.)
+  uint32_t key[EPL];
 #pragma unroll
-    for (int q = 1; q < EPL; ++q) m = fmax(m, c[q]);
-    m = lanes_reduce<LPT>(m, mx);
+  for (int q = 0; q < EPL; ++q) {
+    const uint32_t hi = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, c[q]) >> 32);
+    key[q] = c[q] != c[q] ? 0u : hi ^ ((hi >> 31) ? 0xffffffffu : 0x80000000u);
+  }
+  auto lanes_of = [&](bool p) -> uint64_t {
+    if constexpr (LPT == 64) return __ballot(p);  // (scalar from here on)
+    return (__ballot(p) >> ((threadIdx.x & 63) / LPT * LPT)) & (~0ull >> (64 - LPT));
+  };
+  for (int j = 0; j < a.k; ++j) {
+    uint32_t top = key[0];
+#pragma unroll
+    for (int q = 1; q < EPL; ++q) top = max(top, key[q]);
+    top = lanes_max<LPT>(top);
+    uint64_t bits[EPL];
+    int sharing = 0;
+#pragma unroll
+    for (int q = 0; q < EPL; ++q) {
+      bits[q] = lanes_of(key[q] == top);
+      sharing += __popcll(bits[q]);
+    }
+    if (LPT == 64 ? sharing > 1 : __any(sharing > 1)) {
+      double m = c[0];
+#pragma unroll
+      for (int q = 1; q < EPL; ++q) m = fmax(m, c[q]);
+      m = lanes_reduce<LPT>(m, mx);
+#pragma unroll
+      for (int q = 0; q < EPL; ++q) bits[q] = lanes_of(c[q] == m);
+    }
     bool found = false;
 #pragma unroll
     for (int q = 0; q < EPL; ++q) {
-      const uint64_t bits = (__ballot(c[q] == m) >> shift) & (~0ull >> (64 - LPT));
-      if (!found && bits) {
+      if (!found && bits[q]) {
         found = true;
-        if (l == __builtin_ctzll(bits)) {
+        if (l == __builtin_ctzll(bits[q])) {
           place[q] = j;
           c[q] = kNone;
+          key[q] = 0;
         }
       }
     }
@@ -217,8 +257,9 @@ __device__ __forceinline__ void prefix(int32_t* v, int n, int32_t* wave_sums) {
 
 // Choices of kRouteBlock tokens.  ALONE: they are all there are, and the block
 // finds their places too; else it leaves its count of each expert in ws.
+// (waves per SIMD: two workgroups of 1024 threads have to fit a CU)
 template <int NTH, int LPT, int EPL, bool ALONE>
-__global__ __launch_bounds__(NTH) void route_kernel(RouteArgs a) {
+__global__ __launch_bounds__(NTH, NTH == 1024 && EPL <= 2 ? 8 : 4) void route_kernel(RouteArgs a) {
   extern __shared__ double room[];
   __shared__ unsigned long long mask[kRouteMaxExperts];
   __shared__ int32_t base[kRouteMaxExperts + 1], wave_sums[NTH / 64];
@@ -227,10 +268,20 @@ __global__ __launch_bounds__(NTH) void route_kernel(RouteArgs a) {
   constexpr int kPerPass = NTH / LPT;
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRouteBlock;
   const int n = static_cast<int>(min(static_cast<int64_t>(kRouteBlock), a.T - t0));
-  const int mine = threadIdx.x / LPT;
+  const int mine = threadIdx.x / LPT, l = threadIdx.x % LPT;
+  float z[2][EPL];  // this pass's logits and the next's, which are under way meanwhile
+  auto load = [&](float (&to)[EPL], int i) {
+    const float* row = a.logits + (i < n ? t0 + i : 0) * a.ldl;
+#pragma unroll
+    for (int q = 0; q < EPL; ++q) to[q] = q * LPT + l < a.E ? row[q * LPT + l] : -__builtin_inff();
+  };
+  if (n > 0) load(z[0], mine);
   for (int i0 = 0; i0 < n; i0 += kPerPass) {
     const int i = i0 + mine;
-    route_token<LPT, EPL>(a, t0 + i, i < n, threadIdx.x % LPT, room + mine * (a.E + a.groups), mask, i);
+    if (i0 + kPerPass < n) load(z[1], i + kPerPass);
+    route_token<LPT, EPL>(a, z[0], t0 + i, i < n, l, room + mine * (a.E + a.groups), mask, i);
+#pragma unroll
+    for (int q = 0; q < EPL; ++q) z[0][q] = z[1][q];
   }
   __syncthreads();
   if (!ALONE) {
