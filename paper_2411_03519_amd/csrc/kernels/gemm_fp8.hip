@@ -475,24 +475,30 @@ __global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args
     static_assert(S::BN == 256, "a workgroup has a group of 128 features");
     float* const top = reinterpret_cast<float*>(lds);  // [2][BM]
     f32x4 y[TM][HN];
+    auto activate = [&](auto whole) __attribute__((always_inline)) {  // whole: all the wave's rows of W are there
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      float best = 0.f;
+      for (int j = 0; j < TM; ++j) {
+        float best = 0.f;
 #pragma unroll
-      for (int p = 0; p < HN; ++p) {
-        f32x4 gate, up;
-        gate_and_up(acc[2 * p][j], acc[2 * p + 1][j], gate, up);
-        const bool in = nw + 32 * p < a.N;
+        for (int p = 0; p < HN; ++p) {
+          f32x4 gate, up;
+          gate_and_up(acc[2 * p][j], acc[2 * p + 1][j], gate, up);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          y[j][p][i] = in ? silu_f32(gate[i]) * up[i] : 0.f;
-          best = fmaxf(best, fabsf(y[j][p][i]));
+          for (int i = 0; i < 4; ++i) {
+            y[j][p][i] = silu_f32(gate[i]) * up[i];
+            if (!decltype(whole)::value) y[j][p][i] = nw + 32 * p < a.N ? y[j][p][i] : 0.f;
+            best = fmaxf(best, fabsf(y[j][p][i]));
+          }
         }
+        best = max_xor32(max_xor16(best));
+        if (g == 0) top[wn * S::BM + (wm * TM + j) * 16 + r16] = best;
+        __builtin_amdgcn_sched_barrier(0);
       }
-      __builtin_amdgcn_sched_barrier(0);
-      best = max_xor32(max_xor16(best));
-      if (g == 0) top[wn * S::BM + (wm * TM + j) * 16 + r16] = best;
-    }
+    };
+    if (nw + 16 * TN <= a.N)
+      activate(std::true_type{});
+    else
+      activate(std::false_type{});
     __syncthreads();
     const int F = a.N / 2, f = nw / 2 + 16 * g;
 #pragma unroll
