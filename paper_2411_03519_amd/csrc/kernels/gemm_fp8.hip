@@ -161,6 +161,16 @@ __device__ __forceinline__ void lds_load4s(const void* base, uint32_t off, uint3
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds_base)
                : "memory", "m0");
 }
+// The end of a half: what it read from LDS is in registers everywhere.  Scales
+// that a vector instruction shifted meanwhile are two wait states old.
+__device__ __forceinline__ void half_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_nop 1\n\ts_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+// The same behind the last matrix instruction, with the 8 wait states after which
+// its accumulator may be read.  (In place of half_barrier inside the loop it cost
+// 1.5% at 8192 x 28672 x 16384.)
 __device__ __forceinline__ void drained_barrier() {
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_nop 7\n\ts_barrier" ::: "memory");
@@ -180,7 +190,11 @@ __device__ __forceinline__ int xcd_run(int b, int total) {
 }
 
 // Tile t of mb row blocks x nb column tiles: groups of GM row blocks, rows
-// fastest within a group, so that tiles in flight share X and W tiles.
+// fastest within a group, so that tiles in flight share X and W tiles: an XCD's 32
+// 256 x 256 tiles cover 8 x 4.  (GM 2 / 4 / 8 / 16, us: 8192 x 28672 x 4096 757 / 735 /
+// 723 / 756; eight experts' down of 8192 rows 454 / 434 / 425 / 429; QKV at 301 rows in
+// blocks of 64 16.8 / 16.1 / 14.6 / 14.5.)
+constexpr int kGroupRows = 8;
 template <int GM>
 __device__ __forceinline__ void tile_at(int t, int mb, int nb, int& bm, int& bn) {
   const int group = t / (GM * nb), first = group * GM, gm = min(mb - first, GM), in = t % (GM * nb);
@@ -228,7 +242,7 @@ __global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args
   int bm, bn, e, m0, m1;
   const int item = xcd_run(blockIdx.x, items);
   const int slice = item / (mb * nb);
-  tile_at<4>(item % (mb * nb), mb, nb, bm, bn);
+  tile_at<kGroupRows>(item % (mb * nb), mb, nb, bm, bn);
   if (!row_block(a, bm, S::BM, e, m0, m1)) return;
   e = __builtin_amdgcn_readfirstlane(e);
   m0 = __builtin_amdgcn_readfirstlane(m0);
@@ -405,7 +419,7 @@ __global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args
     half(par, std::integral_constant<int, 0>{}, w_read, x_read, wbase + s0 * 2048, wdst + w_put, xbase + s0 * kGroup,
          xdst + x_put);
     turn();
-    drained_barrier();
+    half_barrier();
     half(par, std::integral_constant<int, 1>{}, w_read, x_read, wbase + s1 * 2048, wdst + w_put, xbase + s1 * kGroup,
          xdst + x_put);
     turn();
@@ -424,7 +438,7 @@ __global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args
 #pragma unroll
       for (int j = 0; j < TM; ++j) sx[j] = static_cast<uint32_t>(sx[j]) >> 8;
     }
-    drained_barrier();
+    half_barrier();
   };
   for (int s = 0; s < nk; s += 2) {
     stage(std::integral_constant<int, 0>{}, s);
