@@ -801,65 +801,65 @@ double expected_blocks(const GemmFp8Args& a, int BM) {
   return std::max<double>(live, static_cast<double>(a.M) / BM + 0.5 * live);
 }
 
-// us that a plan is expected to take: the launch, the larger of the rounds of
-// workgroups and the stream of the weights, and what k slices cost behind it.
+// us that a plan is expected to take: the launch, the rounds of workgroups and the
+// stream of the weights (which overlap, not freely), and what k slices cost
+// behind them.
 double expected_us(const GemmFp8Args& a, int epilogue, const GemmFp8Plan& p) {
   constexpr double kLaunch = 3.0;
+  constexpr int kCus = 256;
+  const bool tiled = p.kind == GemmFp8Kind::kTiled;
   const int ks = std::max(p.ks, 1), stages = (a.Kp / kGroup + ks - 1) / ks;
   const int live = a.offsets ? std::min(a.E, a.M) : 1;  // matrices that have rows
-  const double finish = p.ks ? 2.6 + 8e-6 * ks * a.M * a.N / 5.0 : 0.0;
-  const int bm = 16 * p.mt * (p.kind == GemmFp8Kind::kTiled ? 2 : 1), bn = p.kind == GemmFp8Kind::kTiled ? 32 * p.nt : 32;
-  const double blocks = expected_blocks(a, bm) * ((a.N + bn - 1) / bn) * ks;
-  // MB; row blocks that read the same weights share them in the caches in part
-  const double weights = 1e-6 * a.N * a.Kp * (live + 0.6 * (expected_blocks(a, bm) - live));
-  if (p.kind == GemmFp8Kind::kStream) return kLaunch + weights / std::min(p.mt == 1 ? 5.2 : 4.0, 0.02 * blocks) + finish;
-  constexpr int kCus = 256;
-  // (how the rows of experts fall into rounds is not known)
-  double rounds = a.offsets ? std::max(1.0, blocks / kCus + 0.5) : std::ceil(blocks / kCus);
-  if (rounds > 1 && p.nt == 4 && p.mt <= 4) rounds *= 0.85;  // two workgroups share a CU
-  const double stage = 0.25 + 0.018 * p.nt * p.mt;
-  const double gate = epilogue == kEpi8SwiGLU && !p.ks ? 0.5 * p.mt : 0.0;
-  const double c = rounds * (stages * stage + gate), h = weights / std::min(5.6, 0.03 * blocks);
-  return kLaunch + std::sqrt(std::sqrt(c * c * c * c + h * h * h * h)) + finish;  // (overlapped, not freely)
+  const double finish = p.ks ? 3.9 + 8e-6 * ks * a.M * a.N / 6.8 : 0.0;
+  const int bm = 16 * p.mt * (tiled ? 2 : 1), bn = 16 * p.nt * (tiled ? 2 : 1);
+  const double row_blocks = expected_blocks(a, bm), blocks = row_blocks * ((a.N + bn - 1) / bn) * ks;
+  // MB; further row blocks of the same weights find most of them in the caches
+  const double weights = 1e-6 * a.N * a.Kp * (live + 0.11 * (row_blocks - live));
+  if (!tiled) return kLaunch + weights / std::min(p.mt == 1 ? 5.3 : 3.0, 0.027 * blocks) + finish;
+  double rounds = std::ceil(blocks / kCus);
+  if (a.offsets) {  // the number of blocks is a guess: a round begun counts by how sure it is
+    const double some = blocks / kCus + 0.07, whole = std::floor(some);
+    rounds = std::max(1.0, whole + std::min(1.0, 3.5 * (some - whole)));
+  }
+  const double gate = epilogue == kEpi8SwiGLU && !p.ks ? 0.64 * p.mt : 0.0;
+  const double c = rounds * (stages * (0.25 + 0.011 * p.nt * p.mt) + gate), h = weights / std::min(6.2, 0.042 * blocks);
+  return kLaunch + std::sqrt(std::sqrt(c * c * c * c + h * h * h * h)) + finish;
 }
 
 // Whether W should pass the caches by.  It gains where W streams from HBM and few
 // row blocks read each matrix, more so by experts, whose row blocks of one
 // matrix are neighbours in time (W kept / passed, us): 8B gate/up at 128 / 301 /
 // 1001 rows 33.0 / 29.9, 45.0 / 43.3, 106.7 / 104.1, at 4096 377 / 388; 70B down at 128
-// rows 55.2 / 54.0, at 301 (two row blocks) 87.0 / 90.5; QKV of 4096 x 4096 at 301
-// rows, kept between calls, 14.3 / 17.8; eight experts' gate/up of 50 rows 168.9 /
+// rows 55.2 / 54.0, at 301 (two row blocks) 87.0 / 90.5; a product of 4096 x 4096 at
+// 301 rows, kept between calls, 14.3 / 17.8; eight experts' gate/up of 50 rows 168.9 /
 // 156.5, of 2000 362 / 355, their down of 50 80.5 / 70.6, of 8192 448 / 426.
 bool passes_caches(const GemmFp8Args& a, const GemmFp8Plan& p) {
   const int live = a.offsets ? std::min(a.E, a.M) : 1;
   const double per = expected_blocks(a, 32 * p.mt) / live;
-  return 1e-6 * a.N * a.Kp * live >= 64 && per <= (a.offsets ? 6 : a.N >= 16384 ? 4 : 1);
+  return 1e-6 * a.N * a.Kp * live >= 96 && per <= (a.offsets ? 5.6 : a.N >= 16384 ? 8 : 1);
 }
 
 }  // namespace
 
 // Kernel and k slices: of the plans that the shape and the workspace allow, the
-// one with the least expected time.  What the expectation knows was measured with
-// weights out of the caches, us:
-//  - a tiled stage (128 columns) takes about 0.25 + 0.018 TN TM of a CU, LDS and
-//    barriers first, the matrix cores from TN TM = 48 on: 16 x 32 row tiles (TN, TM)
-//    = 4, 2 0.42; 4, 4 0.54; 4, 8 0.77; 8, 2 0.55; 8, 4 0.79; 8, 6 1.1; 8, 8 1.4.  So
-//    rows are not rounded up to large tiles (8B gate/up at 301 rows as 256 x 256 /
-//    256 x 192 / 256 x 128 tiles 53.6 / 43.2 / 59.6, at 200 rows 48.5 / 43.8 / 37.4),
-//    and rounds of 256 workgroups count whole (8192 rows of 8 experts' down as 256 x
-//    256 / 256 x 192 477 / 449).
-//  - weights stream at 5.6 TB/s where enough workgroups ask: 8B gate/up at 25 rows as
-//    112 workgroups of 256 W rows with SwiGLU in place 31.4, as 224 of 128 with the
-//    finishing launch 25.8.
-//    Further row blocks of the same weights cost about half of it each: 70B down at
-//    128 rows as 2 x 64 rows in 2 slices 70.2, as 128 in 4 55.6; eight experts' gate/up
-//    of 2000 rows in blocks of 128 / 256 361 / 291.
+// one with the least expected time.  The expectation's constants are fitted to
+// the times of all plans of 175 products of 1 to 10000 rows (the 8B, 70B and tiny
+// widths, 4 to 32 experts, weights out of the caches); over those the chosen plan
+// is 2% slower than the best one in the mean, 19% at most.  What they say, us:
+//  - a tiled stage (128 columns) costs 0.25 + 0.011 TN TM of a CU, LDS and barriers
+//    first, the matrix cores from TN TM = 48 on, so rows are not rounded up to
+//    large tiles (8B gate/up at 301 rows as 256 x 256 / 256 x 192 / 256 x 128 tiles
+//    53.6 / 43.2 / 59.6, at 200 rows 48.5 / 43.8 / 37.4), and rounds of 256 workgroups
+//    count whole (8192 rows of 8 experts' down as 256 x 256 / 256 x 192 477 / 438).
+//  - weights stream at 6.2 TB/s where enough workgroups ask: 8B gate/up at 25 rows as
+//    112 workgroups of 256 W rows with SwiGLU in place 27.8, as 224 of 128 with the
+//    finishing launch 24.2.
 //  - k slices fill the CUs of narrow products and cost a launch and their sums'
-//    traffic: 70B down at 128 rows in 1 / 2 / 4 / 8 slices of 128 x 128 tiles 121 / 72 /
-//    55.6 / 64, QKV at 301 rows in 1 / 2 16.4 / 21.3.
+//    traffic: 70B down at 128 rows in 1 / 2 / 4 / 8 slices of 128 x 128 tiles 113 / 86 /
+//    57 / 64, QKV at 301 rows in 1 / 2 14.9 / 21.0.
 //  - up to 32 rows (of each expert) the streaming kernel keeps a narrow product of
 //    few bytes in flight at once: QKV at 25 rows 8.4 against 10.9 of 4 tiled slices,
-//    8B down at 16 rows 15.9 / 17.8, but 70B QKV at 32 rows 26.9 / 23.6.
+//    8B down at 16 rows 15.8 / 17.5, but 70B QKV at 32 rows 26.9 / 23.6.
 GemmFp8Plan plan_gemm_fp8(const GemmFp8Args& a, int epilogue) {
   // The tiled kernel reaches rows by 32-bit byte offsets from its block's first
   // element, or from the first row of X where rows are gathered.
@@ -885,7 +885,7 @@ GemmFp8Plan plan_gemm_fp8(const GemmFp8Args& a, int epilogue) {
       if (ks || !swiglu) offer({GemmFp8Kind::kTiled, 4, mt, ks, false});
       if (ks != 1) offer({GemmFp8Kind::kTiled, 8, mt, ks, false});
     }
-    if (a.M <= 32 * (a.offsets ? a.E : 1) && (ks || !swiglu)) offer({GemmFp8Kind::kStream, 2, a.M <= 16 * a.E ? 1 : 2, ks, false});
+    if (a.M <= 32 * a.E && (ks || !swiglu)) offer({GemmFp8Kind::kStream, 2, a.M <= 16 * a.E ? 1 : 2, ks, false});
   }
   best.nt_hint = best.kind == GemmFp8Kind::kTiled && passes_caches(a, best);
   return best;
