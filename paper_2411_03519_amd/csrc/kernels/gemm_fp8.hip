@@ -161,16 +161,16 @@ __device__ __forceinline__ void lds_load4s(const void* base, uint32_t off, uint3
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds_base)
                : "memory", "m0");
 }
-// The end of a half: what it read from LDS is in registers everywhere.  Scales
-// that a vector instruction shifted meanwhile are two wait states old.
+// The end of a half: what it read from LDS is in registers everywhere.
 __device__ __forceinline__ void half_barrier() {
   __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_nop 1\n\ts_barrier" ::: "memory");
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
-// The same behind the last matrix instruction, with the 8 wait states after which
-// its accumulator may be read.  (In place of half_barrier inside the loop it cost
-// 1.5% at 8192 x 28672 x 16384.)
+// The end of a stage: also 8 wait states, behind which the last matrix
+// instruction's accumulator may be read (the loop may end here) and the scales
+// that vector instructions shifted may be operands.  (Behind both halves of a stage
+// it cost 1.5% at 8192 x 28672 x 16384.)
 __device__ __forceinline__ void drained_barrier() {
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_nop 7\n\ts_barrier" ::: "memory");
@@ -438,7 +438,7 @@ __global__ __launch_bounds__(256, S::OCC) void gemm_fp8_tiled_kernel(GemmFp8Args
 #pragma unroll
       for (int j = 0; j < TM; ++j) sx[j] = static_cast<uint32_t>(sx[j]) >> 8;
     }
-    half_barrier();
+    drained_barrier();
   };
   for (int s = 0; s < nk; s += 2) {
     stage(std::integral_constant<int, 0>{}, s);
@@ -873,6 +873,8 @@ GemmFp8Plan plan_gemm_fp8(const GemmFp8Args& a, int epilogue) {
   double least = expected_us(a, epilogue, best);
   auto offer = [&](GemmFp8Plan p) {
     if (p.ks > units || static_cast<int64_t>(p.ks) * a.M * a.N > a.ws_floats) return;
+    const int bm = 16 * p.mt * (p.kind == GemmFp8Kind::kTiled ? 2 : 1), bn = 16 * p.nt * (p.kind == GemmFp8Kind::kTiled ? 2 : 1);
+    if (static_cast<int64_t>(row_blocks(a, bm)) * ((a.N + bn - 1) / bn) * std::max(p.ks, 1) >= (1 << 23)) return;  // (2^32 threads)
     const double t = expected_us(a, epilogue, p);
     if (t < least) {
       least = t;

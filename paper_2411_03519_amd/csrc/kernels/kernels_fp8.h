@@ -44,6 +44,7 @@ hipError_t launch_combine(const CombineArgs& a, hipStream_t s);
 constexpr int kRouteMaxExperts = 512;
 constexpr int kRouteMaxTopK = 32;
 constexpr int kRouteMaxGroups = 64;
+constexpr int kRouteMaxTokens = 1 << 24;  // (times kRouteMaxTopK within 31 bits)
 constexpr int kRouteBlock = 64;  // tokens whose places in the experts' rows one workgroup finds
 
 struct RouteArgs {
@@ -70,6 +71,8 @@ enum GemmFp8Epilogue {
 // Dense (offsets null): rows m = 0 .. M-1 of X with one W.  By experts: slots
 // offsets[e] .. offsets[e + 1] - 1 (within 0 .. M) take W + e * N * Kp, slot m
 // row src[m] of X (row m where src is null).
+constexpr int kGemmFp8MaxRows = 1 << 26, kGemmFp8MaxExperts = 1024;
+constexpr int64_t kGemmFp8MaxOut = int64_t{1} << 36;  // results: workgroups of any plan that is chosen fit a grid
 struct GemmFp8Args {
   const uint8_t* X;        // [x_rows][ldx] e4m3
   const uint8_t* x_scale;  // [x_rows][ldxs]

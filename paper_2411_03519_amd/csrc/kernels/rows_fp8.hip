@@ -11,72 +11,74 @@ namespace metro {
 
 // ---------------------------------------------------------------------------
 // x' = x + delta;  h = x' * rsqrt(mean(x'^2) + eps) * g;  h to 8-bit rows.
-// One block per row; a thread holds VPT float4 of it, 32 neighbouring lanes one
-// group of 128.  The norm is fp32 and the codes are rounded from its fp32 values
+// One block per row (more rows than blocks: every gridDim-th); a thread holds VPT
+// float4 of it, 32 neighbouring lanes one group of 128.  The norm is fp32 and the codes are rounded from its fp32 values
 // (not from the optional bf16 ones).
 // ---------------------------------------------------------------------------
 template <int NTH, int VPT>
 __global__ __launch_bounds__(NTH) void rmsnorm_fp8_kernel(NormFp8Args a) {
-  const int64_t r = blockIdx.x;
-  const int n4 = a.d / 4, pad4 = (a.d + kGroup - 1) / kGroup * (kGroup / 4);
-  const float4* xr = reinterpret_cast<const float4*>(a.x + r * a.ldx);
-  const uint2* dr = reinterpret_cast<const uint2*>(a.delta + r * a.ldd);
-  const uint2* gr = reinterpret_cast<const uint2*>(a.gain);
-  float4 v[VPT];
-  uint2 gw[VPT];
-#pragma unroll
-  for (int j = 0; j < VPT; ++j) {
-    const int i = threadIdx.x + j * NTH;
-    v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-    gw[j] = make_uint2(0, 0);
-    if (i < n4) {
-      v[j] = xr[i];
-      gw[j] = gr[i];
-    }
-  }
-  if (a.delta) {
-    float4* xo = reinterpret_cast<float4*>(a.x_out + r * a.ldx);
+  constexpr int NWV = NTH / 64;
+  __shared__ float red[NWV];
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const int n4 = a.d / 4, pad4 = (a.d + kGroup - 1) / kGroup * (kGroup / 4);
+    const float4* xr = reinterpret_cast<const float4*>(a.x + r * a.ldx);
+    const uint2* dr = reinterpret_cast<const uint2*>(a.delta + r * a.ldd);
+    const uint2* gr = reinterpret_cast<const uint2*>(a.gain);
+    float4 v[VPT];
+    uint2 gw[VPT];
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
       const int i = threadIdx.x + j * NTH;
-      if (i >= n4) continue;
-      const uint2 dw = dr[i];
-      v[j].x += lo_bf16(dw.x);
-      v[j].y += hi_bf16(dw.x);
-      v[j].z += lo_bf16(dw.y);
-      v[j].w += hi_bf16(dw.y);
-      if (a.x_out) xo[i] = v[j];
+      v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+      gw[j] = make_uint2(0, 0);
+      if (i < n4) {
+        v[j] = xr[i];
+        gw[j] = gr[i];
+      }
     }
-  }
-  float ss = 0.f;
+    if (a.delta) {
+      float4* xo = reinterpret_cast<float4*>(a.x_out + r * a.ldx);
 #pragma unroll
-  for (int j = 0; j < VPT; ++j) ss += v[j].x * v[j].x + v[j].y * v[j].y + v[j].z * v[j].z + v[j].w * v[j].w;
-  ss = wave_sum(ss);
-  constexpr int NWV = NTH / 64;
-  __shared__ float red[NWV];
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
-  __syncthreads();
-  float tot = 0.f;
+      for (int j = 0; j < VPT; ++j) {
+        const int i = threadIdx.x + j * NTH;
+        if (i >= n4) continue;
+        const uint2 dw = dr[i];
+        v[j].x += lo_bf16(dw.x);
+        v[j].y += hi_bf16(dw.x);
+        v[j].z += lo_bf16(dw.y);
+        v[j].w += hi_bf16(dw.y);
+        if (a.x_out) xo[i] = v[j];
+      }
+    }
+    float ss = 0.f;
 #pragma unroll
-  for (int w = 0; w < NWV; ++w) tot += red[w];
-  const float inv = rsqrtf(tot / static_cast<float>(a.d) + a.eps);
-  uint32_t* hr = reinterpret_cast<uint32_t*>(a.h + r * a.ldh);
+    for (int j = 0; j < VPT; ++j) ss += v[j].x * v[j].x + v[j].y * v[j].y + v[j].z * v[j].z + v[j].w * v[j].w;
+    ss = wave_sum(ss);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
+    __syncthreads();
+    float tot = 0.f;
 #pragma unroll
-  for (int j = 0; j < VPT; ++j) {
-    const int i = threadIdx.x + j * NTH;
-    if (i >= pad4) continue;  // (whole groups of 32 lanes)
-    const float4 h = make_float4(v[j].x * inv * lo_bf16(gw[j].x), v[j].y * inv * hi_bf16(gw[j].x),
-                                 v[j].z * inv * lo_bf16(gw[j].y), v[j].w * inv * hi_bf16(gw[j].y));
-    if (a.h16 && i < n4)
-      reinterpret_cast<uint2*>(a.h16 + r * a.ldh16)[i] = make_uint2(pack_bf16x2(h.x, h.y), pack_bf16x2(h.z, h.w));
-    float m = fmaxf(fmaxf(fabsf(h.x), fabsf(h.y)), fmaxf(fabsf(h.z), fabsf(h.w)));
+    for (int w = 0; w < NWV; ++w) tot += red[w];
+    const float inv = rsqrtf(tot / static_cast<float>(a.d) + a.eps);
+    uint32_t* hr = reinterpret_cast<uint32_t*>(a.h + r * a.ldh);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 32));
-    const int e = e8m0_of(m);
-    const float s = e8m0_inverse(e);
-    // columns d .. of the last group: zero codes, whatever 0 * inv * 0 is there
-    hr[i] = i < n4 ? pack_e4m3(h.x * s, h.y * s, h.z * s, h.w * s) : 0u;
-    if (threadIdx.x % 32 == 0) a.h_scale[r * a.lds + i / 32] = static_cast<uint8_t>(e);
+    for (int j = 0; j < VPT; ++j) {
+      const int i = threadIdx.x + j * NTH;
+      if (i >= pad4) continue;  // (whole groups of 32 lanes)
+      const float4 h = make_float4(v[j].x * inv * lo_bf16(gw[j].x), v[j].y * inv * hi_bf16(gw[j].x),
+                                   v[j].z * inv * lo_bf16(gw[j].y), v[j].w * inv * hi_bf16(gw[j].y));
+      if (a.h16 && i < n4)
+        reinterpret_cast<uint2*>(a.h16 + r * a.ldh16)[i] = make_uint2(pack_bf16x2(h.x, h.y), pack_bf16x2(h.z, h.w));
+      float m = fmaxf(fmaxf(fabsf(h.x), fabsf(h.y)), fmaxf(fabsf(h.z), fabsf(h.w)));
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 32));
+      const int e = e8m0_of(m);
+      const float s = e8m0_inverse(e);
+      // columns d .. of the last group: zero codes, whatever 0 * inv * 0 is there
+      hr[i] = i < n4 ? pack_e4m3(h.x * s, h.y * s, h.z * s, h.w * s) : 0u;
+      if (threadIdx.x % 32 == 0) a.h_scale[r * a.lds + i / 32] = static_cast<uint8_t>(e);
+    }
+    if (r + gridDim.x < a.rows) __syncthreads();  // (red is read)
   }
 }
 
@@ -85,7 +87,7 @@ hipError_t launch_rmsnorm_fp8(const NormFp8Args& a, hipStream_t s) {
   const int pad4 = (a.d + kGroup - 1) / kGroup * (kGroup / 4);
   auto go = [&](auto nth, auto vpt) {
     constexpr int NTH = decltype(nth)::value, VPT = decltype(vpt)::value;
-    rmsnorm_fp8_kernel<NTH, VPT><<<dim3(a.rows), dim3(NTH), 0, s>>>(a);
+    rmsnorm_fp8_kernel<NTH, VPT><<<dim3(std::min(a.rows, 1 << 21)), dim3(NTH), 0, s>>>(a);
   };
   if (pad4 <= 256)
     go(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});

@@ -31,6 +31,8 @@ metro_status gemm_fp8(const char* who, metro::GemmFp8Args& a, int32_t epilogue, 
     return report(METRO_E_INVAL, "%s: NULL operand or output", who);
   if (a.M < 0 || a.N <= 0 || a.N % 32 || a.Kp <= 0 || a.Kp % 128)
     return report(METRO_E_INVAL, "%s: bad shape (rows >= 0, N %% 32, Kp %% 128 required)", who);
+  if (a.M > metro::kGemmFp8MaxRows || static_cast<int64_t>(a.M) * a.N > metro::kGemmFp8MaxOut || a.E > metro::kGemmFp8MaxExperts)
+    return report(METRO_E_INVAL, "%s: more than 2^26 rows, 2^36 results or %d experts", who, metro::kGemmFp8MaxExperts);
   if (a.ldx < a.Kp || a.ldx % 16 || a.ldxs < (groups_of(a.Kp) + 3) / 4 * 4 || a.ldxs % 4)
     return report(METRO_E_INVAL, "%s: ldx must be a multiple of 16 from Kp on, ldxs one of 4 from Kp / 128 on", who);
   if (swiglu ? a.ldo < groups_of(a.N / 2) * 128 || a.ldo % 16 || a.ldos < groups_of(a.N / 2) : a.ldo < a.N || a.ldo % 4)
@@ -94,7 +96,7 @@ metro_status metro_op_gemm_fp8_plan(int32_t M, int32_t N, int32_t Kp, int32_t ep
                                     int32_t* k_slices) {
   clear_error();
   if (!kind || !w_rows || !x_rows || !k_slices || M <= 0 || N <= 0 || N % 32 || Kp <= 0 || Kp % 128 || n_experts < 0 ||
-      workspace_bytes < 0 || (epilogue != metro::kEpi8Bf16 && epilogue != metro::kEpi8SwiGLU))
+      M > metro::kGemmFp8MaxRows || n_experts > metro::kGemmFp8MaxExperts || workspace_bytes < 0 || (epilogue != metro::kEpi8Bf16 && epilogue != metro::kEpi8SwiGLU))
     return report(METRO_E_INVAL, "gemm_fp8_plan: bad shape (N %% 32, Kp %% 128), epilogue or NULL output");
   static const int32_t some = 0;
   metro::GemmFp8Args a{};
@@ -127,7 +129,7 @@ metro_status metro_op_route(const float* logits, int32_t ldl, const float* bias,
   if (top_k <= 0 || top_k > metro::kRouteMaxTopK || top_k > n_experts / n_groups * top_groups)
     return report(METRO_E_INVAL, "route: top_k must be 1 .. %d and at most the experts of top_groups groups",
                   metro::kRouteMaxTopK);
-  if (static_cast<int64_t>(T) * top_k > INT32_MAX) return report(METRO_E_INVAL, "route: T * top_k passes 2^31 - 1");
+  if (T > metro::kRouteMaxTokens) return report(METRO_E_INVAL, "route: more than %d tokens", metro::kRouteMaxTokens);
   if (misaligned(logits, 4) || misaligned(bias, 4) || misaligned(weights, 4) || misaligned(workspace, 4))
     return report(METRO_E_INVAL, "route: misaligned buffer");
   if (T > metro::kRouteBlock) {

@@ -68,7 +68,7 @@ OPERANDS = (nulls("X", "x_scale", "W", "w_scale") + off(8, "X", "W", "w_scale", 
 
 def test_gemm_refusals(lib):
     refused(lib, "metro_op_gemm_fp8", GEMM, OPERANDS + nulls("out_bf16") + off(4, "out_bf16") +
-            [{"M": -1}, {"ldo": 316}, {"ldo": 322}], b"gemm_fp8")
+            [{"M": -1}, {"M": (1 << 26) + 1}, {"M": 1 << 26, "N": 1056, "ldo": 1056}, {"ldo": 316}, {"ldo": 322}], b"gemm_fp8")
     refused(lib, "metro_op_gemm_fp8", SWIGLU, OPERANDS + nulls("out_fp8", "out_scale") + off(8, "out_fp8") +
             [{"M": -1}, {"ldo": 160}, {"ldo": 264}, {"ldos": 1}], b"gemm_fp8")
 
@@ -83,7 +83,7 @@ def test_experts_refusals(lib):
                 d[k] = v
         return d
 
-    more = nulls("offsets") + [{"n_experts": 0}, {"R": -1}, {"x_rows": 0}, {"x_rows": -1}, {"src": None}]
+    more = nulls("offsets") + [{"n_experts": 0}, {"n_experts": 1025}, {"R": -1}, {"x_rows": 0}, {"x_rows": -1}, {"src": None}]
     refused(lib, "metro_op_gemm_fp8_experts", by_experts(GEMM), OPERANDS + more + nulls("out_bf16"), b"gemm_fp8_experts")
     refused(lib, "metro_op_gemm_fp8_experts", by_experts(SWIGLU), OPERANDS + more + nulls("out_fp8", "out_scale"),
             b"gemm_fp8_experts")
@@ -96,7 +96,7 @@ def test_route_refusals(lib):
     refused(lib, "metro_op_route", good, nulls("logits", "experts", "weights", "offsets", "src", "slot", "workspace") +
             [{"T": -1}, {"ldl": 63}, {"n_experts": 0}, {"n_experts": 513, "ldl": 513}, {"scoring": 2}, {"n_groups": 0},
              {"n_groups": 7}, {"n_groups": 128}, {"top_groups": 0}, {"top_groups": 9}, {"top_k": 0}, {"top_k": 17}, {"top_k": 33},
-             {"workspace_bytes": 4 * 64 * 2 - 1}, {"T": 300_000_000}], b"route")
+             {"workspace_bytes": 4 * 64 * 2 - 1}, {"T": (1 << 24) + 1, "workspace_bytes": 1 << 40}], b"route")
 
 
 def test_combine_refusals(lib):

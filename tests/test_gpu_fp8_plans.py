@@ -1,0 +1,292 @@
+"""Every variant that the 8-bit products' plan can choose, on small whole numbers.
+
+Codes stand for -3 .. 3 and the powers of two spread over 4, so that every partial
+sum stays within 24 bits and no product of eight is cut: results have to equal
+the float64 product, rounded to bf16, bit for bit.  SwiGLU's codes have to be
+those of a value within 2^-17 of the definition's (see test_gpu_fp8_ops.py).
+Each case names the variant that it is there for (kind, W rows and X rows of a
+workgroup, k slices).
+"""
+
+import numpy as np
+import pytest
+
+from oracle import fp8
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def metro():
+    if not torch.cuda.is_available():
+        pytest.skip("no HIP device")
+    from paper_2411_03519_amd import metro as m
+    return m
+
+
+CODES = torch.from_numpy(fp8.e4m3_code(np.arange(-3.0, 4.0)))
+
+
+class Operands:
+    """8-bit rows and weights of whole numbers on the device, and their float64 values."""
+
+    def __init__(self, seed, x_rows, N, K, E=1, down=0):
+        self.g = torch.Generator(device="cuda")
+        self.g.manual_seed(seed)
+        self.x, self.xs, self.xv = self.draw(x_rows, K, 0)
+        self.xs = torch.nn.functional.pad(self.xs, (0, -(K // 128) % 4), value=255).contiguous()
+        self.W, self.ws, self.wv = [], [], []
+        for _ in range(E):
+            codes, byte, v = self.draw(N, K, down)
+            w, b = pack(codes, byte)
+            self.W.append(w)
+            self.ws.append(b)
+            self.wv.append(v)
+        self.W, self.ws = torch.cat(self.W), torch.cat(self.ws)
+
+    def draw(self, rows, K, down):
+        i = torch.randint(0, 7, (rows, K), generator=self.g, device="cuda")
+        byte = torch.randint(127 - down, 129 - down, (rows, K // 128), generator=self.g, device="cuda")
+        v = (i - 3).double() * torch.repeat_interleave(torch.exp2(byte.double() - 127), 128, dim=1)
+        return CODES.cuda()[i], byte.to(torch.uint8), v
+
+
+def pack(codes, byte):
+    N, K = codes.shape
+    w = codes.reshape(N // 16, 16, K // 128, 2, 4, 16).permute(0, 2, 3, 4, 1, 5).contiguous().reshape(-1)
+    b = torch.nn.functional.pad(byte, (0, -(K // 128) % 4), value=255)
+    return w, b.reshape(N // 16, 16, -1, 4).permute(0, 2, 1, 3).contiguous().reshape(-1)
+
+
+def test_pack_of_these_tests_is_the_headers_layout(metro):
+    codes = torch.randint(0, 255, (48, 640), dtype=torch.uint8)
+    byte = torch.randint(0, 255, (48, 5), dtype=torch.uint8)
+    w, b = pack(codes, byte)
+    np.testing.assert_array_equal(w.numpy(), fp8.packed_codes(codes.numpy()))
+    np.testing.assert_array_equal(b.numpy(), fp8.packed_bytes(byte.numpy(), 255))
+
+
+def swiglu(y):
+    b = y.reshape(y.shape[0], y.shape[1] // 16, 2, 8)
+    return (b[:, :, 0] / (1 + torch.exp(-b[:, :, 0])) * b[:, :, 1]).reshape(y.shape[0], y.shape[1] // 2)
+
+
+def check_rows8(codes, byte, want, slack=2.0 ** -17):
+    """As in test_gpu_fp8_ops.py, in torch: codes and powers are those of values within `slack` of want."""
+    rows, n = want.shape
+    G = -(-n // 128)
+    q = torch.nn.functional.pad(want, (0, G * 128 - n)).reshape(rows, G, 128)
+    top = q.abs().amax(2)
+
+    def power(t):  # the smallest 2^e with t <= 448 * 2^e
+        m, e = torch.frexp(t / 448.0)
+        return torch.where(t > 0, (e + 127 - (m == 0.5).int()).clamp(min=1), torch.ones_like(e))
+
+    byte = byte[:, :G].int()
+    assert bool(((byte >= power(top * (1 - slack))) & (byte <= power(top * (1 + slack)))).all())
+    p = torch.exp2(byte.double() - 127).unsqueeze(2)
+    got = codes[:, :G * 128].contiguous().view(torch.float8_e4m3fn).double().reshape(q.shape)
+
+    def rounded(v):
+        v = (v / p).clamp(-448, 448)
+        step = torch.exp2(torch.floor(torch.log2(v.abs().clamp(min=2.0 ** -6))) - 3)
+        return torch.round(v / step) * step
+
+    a, b = rounded(q * (1 - slack)), rounded(q * (1 + slack))
+    assert bool(((got >= torch.minimum(a, b)) & (got <= torch.maximum(a, b))).all())
+
+
+def same_bf16(out, y):
+    return bool((out.view(torch.bfloat16).double() == y.float().to(torch.bfloat16).double()).all())
+
+
+def counts_of(M, E):
+    """Ragged counts of M slots: one expert empty, the rest uneven."""
+    first = M // 2
+    return [first, 0, M - first] + [0] * (E - 3)
+
+
+def run(metro, M, N, K, epilogue, E, ws):
+    o = Operands(M + N, M, N, K, max(E, 1), 6 if epilogue == 2 else 0)
+    workspace = torch.full((ws * M * N,), float("nan"), device="cuda") if ws else None
+    G = -(-(N // 2) // 128)
+    if epilogue == 2:
+        out = torch.full((M + 1, G * 128), 0xA5, dtype=torch.uint8, device="cuda")
+        scale = torch.full((M + 1, -(-G // 4) * 4), 0xA5, dtype=torch.uint8, device="cuda")
+    else:
+        out, scale = torch.full((M + 1, N), 77, dtype=torch.int16, device="cuda"), None
+    if E:
+        counts = counts_of(M, E)
+        offsets = [int(v) for v in np.concatenate([[0], np.cumsum(counts)])]
+        src = torch.randperm(M, generator=o.g, device="cuda")
+        metro.op_gemm_fp8_experts(o.x, o.xs, M, src.int(), torch.tensor(offsets, dtype=torch.int32, device="cuda"), E, M, o.W,
+                                  o.ws, N, K, epilogue, out, out_scale=scale, workspace=workspace)
+        y = torch.cat([o.xv[src[offsets[e]:offsets[e + 1]]] @ o.wv[e].t() for e in range(E)])
+    else:
+        metro.op_gemm_fp8(o.x, o.xs, o.W, o.ws, M, N, K, epilogue, out, out_scale=scale, workspace=workspace)
+        y = o.xv @ o.wv[0].t()
+    if epilogue == 2:
+        check_rows8(out[:M], scale[:M], swiglu(y))
+        assert bool((out[M] == 0xA5).all() and (scale[M] == 0xA5).all())
+    else:
+        assert same_bf16(out[:M], y)
+        assert bool((out[M] == 77).all())
+
+
+# (rows, N, K, epilogue, experts (0: dense), workspace in slices, kind, W rows, X rows, k slices)
+VARIANTS = [
+(1, 32, 640, 0, 0, 8, "stream", 32, 16, 0),
+    (1, 32, 640, 0, 3, 0, "stream", 32, 16, 0),
+    (1, 6272, 896, 2, 0, 8, "stream", 32, 16, 1),
+    (1, 6272, 896, 2, 3, 8, "stream", 32, 16, 1),
+    (1, 32, 4736, 0, 0, 8, "stream", 32, 16, 8),
+    (1, 32, 4736, 0, 3, 8, "stream", 32, 16, 8),
+    (1, 32, 1152, 2, 0, 8, "stream", 32, 16, 2),
+    (1, 32, 1152, 2, 3, 8, "stream", 32, 16, 2),
+    (17, 32, 640, 0, 0, 8, "stream", 32, 32, 0),
+    (49, 32, 640, 0, 3, 0, "stream", 32, 32, 0),
+    (18, 3392, 896, 2, 0, 8, "stream", 32, 32, 1),
+    (56, 1056, 896, 2, 3, 8, "stream", 32, 32, 1),
+    (17, 32, 4736, 0, 0, 8, "stream", 32, 32, 8),
+    (53, 32, 4736, 0, 3, 8, "stream", 32, 32, 8),
+    (17, 32, 1152, 2, 0, 8, "stream", 32, 32, 2),
+    (49, 32, 1152, 2, 3, 8, "stream", 32, 32, 2),
+    (134, 11040, 640, 0, 0, 8, "tiled", 128, 128, 0),
+    (125, 9248, 640, 0, 3, 8, "tiled", 128, 128, 0),
+    (2061, 32, 4736, 0, 0, 8, "tiled", 128, 128, 8),
+    (1961, 32, 4736, 0, 3, 8, "tiled", 128, 128, 8),
+    (2055, 32, 4736, 2, 0, 8, "tiled", 128, 128, 8),
+    (2112, 32, 4736, 2, 3, 8, "tiled", 128, 128, 8),
+    (258, 13536, 640, 0, 0, 0, "tiled", 128, 192, 0),
+    (258, 9312, 640, 0, 3, 0, "tiled", 128, 192, 0),
+    (2069, 160, 4736, 0, 0, 8, "tiled", 128, 192, 8),
+    (1938, 160, 4736, 0, 3, 8, "tiled", 128, 192, 8),
+    (2095, 160, 4736, 2, 0, 8, "tiled", 128, 192, 8),
+    (1941, 160, 4736, 2, 3, 8, "tiled", 128, 192, 8),
+    (385, 12288, 640, 0, 0, 0, "tiled", 128, 256, 0),
+    (359, 9760, 640, 0, 3, 0, "tiled", 128, 256, 0),
+    (193, 2208, 8960, 0, 0, 8, "tiled", 128, 256, 8),
+    (2923, 160, 8960, 0, 3, 8, "tiled", 128, 256, 8),
+    (215, 2080, 8960, 2, 0, 8, "tiled", 128, 256, 8),
+    (2972, 160, 8960, 2, 3, 8, "tiled", 128, 256, 8),
+    (33, 32, 640, 0, 0, 0, "tiled", 128, 64, 0),
+    (97, 32, 640, 0, 3, 8, "tiled", 128, 64, 0),
+    (58, 7424, 1792, 2, 3, 8, "tiled", 128, 64, 1),
+    (33, 32, 2688, 0, 0, 8, "tiled", 128, 64, 4),
+    (97, 32, 2688, 0, 3, 8, "tiled", 128, 64, 4),
+    (33, 32, 1408, 2, 0, 8, "tiled", 128, 64, 2),
+    (101, 32, 1408, 2, 3, 8, "tiled", 128, 64, 2),
+    (530, 11200, 640, 0, 0, 8, "tiled", 256, 128, 0),
+    (166, 14176, 640, 0, 3, 8, "tiled", 256, 128, 0),
+    (2750, 1312, 640, 2, 0, 0, "tiled", 256, 128, 0),
+    (234, 14176, 640, 2, 3, 8, "tiled", 256, 128, 0),
+    (65, 4384, 11520, 0, 0, 8, "tiled", 256, 128, 8),
+    (266, 1472, 12928, 0, 3, 8, "tiled", 256, 128, 8),
+    (69, 4224, 8960, 2, 0, 8, "tiled", 256, 128, 8),
+    (219, 1600, 12928, 2, 3, 8, "tiled", 256, 128, 8),
+    (537, 13152, 640, 0, 0, 0, "tiled", 256, 192, 0),
+    (368, 15040, 640, 0, 3, 0, "tiled", 256, 192, 0),
+    (2973, 2592, 640, 2, 0, 8, "tiled", 256, 192, 0),
+    (480, 14880, 640, 2, 3, 8, "tiled", 256, 192, 0),
+    (967, 11264, 640, 0, 0, 0, "tiled", 256, 256, 0),
+    (554, 14784, 640, 0, 3, 0, "tiled", 256, 256, 0),
+    (842, 13088, 640, 2, 0, 8, "tiled", 256, 256, 0),
+    (857, 11104, 640, 2, 3, 0, "tiled", 256, 256, 0),
+    (271, 11104, 640, 0, 0, 0, "tiled", 256, 64, 0),
+    (3, 12160, 640, 0, 3, 0, "tiled", 256, 64, 0),
+    (1, 32, 640, 2, 0, 8, "tiled", 256, 64, 0),
+    (1, 32, 640, 2, 3, 8, "tiled", 256, 64, 0),
+    (1, 4128, 8960, 0, 0, 8, "tiled", 256, 64, 8),
+    (2, 2080, 8960, 0, 3, 8, "tiled", 256, 64, 8),
+    (1, 8608, 1792, 2, 0, 8, "tiled", 256, 64, 4),
+    (3, 3008, 1792, 2, 3, 8, "tiled", 256, 64, 4),
+    # weights past the caches (from 96 MB on)
+    (40, 28672, 4096, 2, 0, 8, "tiled", 128, 64, 1),
+    (120, 28672, 4096, 2, 0, 0, "tiled", 256, 64, 0),
+    (300, 28672, 4096, 2, 0, 0, "tiled", 256, 192, 0),
+    (90, 8192, 14336, 0, 0, 8, "tiled", 128, 128, 4),
+    (60, 14336, 4096, 0, 3, 0, "tiled", 256, 64, 0),
+]
+
+
+@pytest.mark.parametrize("M,N,K,epilogue,E,ws,kind,w_rows,x_rows,ks", VARIANTS)
+def test_variant(metro, M, N, K, epilogue, E, ws, kind, w_rows, x_rows, ks):
+    assert metro.op_gemm_fp8_plan(M, N, K, epilogue, E, 4 * ws * M * N) == (kind, w_rows, x_rows, ks)
+    run(metro, M, N, K, epilogue, E, ws)
+
+
+# --- buffers past 32 bits ------------------------------------------------------------
+
+
+def test_rows_too_far_apart_for_32_bit_offsets(metro):
+    """X rows 1 GiB apart, gathered, and 17 MiB apart, dense: the direct kernel, both epilogues."""
+    K, N = 256, 288
+    for ldx, M, gathered in ((1 << 30, 6, True), (17 << 20, 40, False)):
+        o = Operands(1, M, N, K, 1, 6)
+        X = torch.empty((M - 1) * ldx + K, dtype=torch.uint8, device="cuda")
+        for i in range(M):
+            X[i * ldx:i * ldx + K] = o.x[i]
+        y = o.xv @ o.wv[0].t()
+        out = torch.zeros(M, N, dtype=torch.int16, device="cuda")
+        codes, scale = (torch.full((M, n), 0xA5, dtype=torch.uint8, device="cuda") for n in (256, 4))
+        for epi, buf in ((0, out), (2, codes)):
+            kw = dict(out_scale=scale if epi else None, ldx=ldx)
+            if gathered:
+                src = torch.arange(M, dtype=torch.int32, device="cuda")
+                off = torch.tensor([0, M], dtype=torch.int32, device="cuda")
+                metro.op_gemm_fp8_experts(X, o.xs, M, src, off, 1, M, o.W, o.ws, N, K, epi, buf, **kw)
+            else:
+                metro.op_gemm_fp8(X, o.xs, o.W, o.ws, M, N, K, epi, buf, **kw)
+        assert same_bf16(out, y)
+        check_rows8(codes, scale, swiglu(y))
+        del X
+
+
+@pytest.mark.parametrize("M,ws", [(20, 0), (70, 8), (200, 0)])
+def test_outputs_past_32_bits(metro, M, ws):
+    N, K, ldo = 288, 384, (1 << 32) // M // 16 * 16 + 64  # elements: the last rows lie past 2^32
+    o = Operands(2, M, N, K, 1, 6)
+    workspace = torch.empty(ws * M * N, device="cuda") if ws else None
+    y = o.xv @ o.wv[0].t()
+    out = torch.empty((M - 1) * ldo + N, dtype=torch.int16, device="cuda")
+    metro.op_gemm_fp8(o.x, o.xs, o.W, o.ws, M, N, K, 0, out, ldo=ldo, workspace=workspace)
+    assert same_bf16(torch.stack([out[i * ldo:i * ldo + N] for i in range(M)]), y)
+    del out
+    out = torch.empty((M - 1) * ldo + 256, dtype=torch.uint8, device="cuda")
+    scale = torch.empty(M, 4, dtype=torch.uint8, device="cuda")
+    metro.op_gemm_fp8(o.x, o.xs, o.W, o.ws, M, N, K, 2, out, out_scale=scale, ldo=ldo, workspace=workspace)
+    check_rows8(torch.stack([out[i * ldo:i * ldo + 256] for i in range(M)]), scale, swiglu(y))
+
+
+def test_weights_of_the_last_expert_past_32_bits(metro):
+    N, K, E = 4096, 14336, 80  # 4.7 GB of weights
+    o = Operands(3, 9, N, K, 1)
+    W = torch.zeros(E * N * K, dtype=torch.uint8, device="cuda")
+    ws = torch.full((E * N * 112,), 127, dtype=torch.uint8, device="cuda")
+    W[-N * K:], ws[-N * 112:] = o.W, o.ws
+    off = torch.zeros(E + 1, dtype=torch.int32, device="cuda")
+    off[E] = 9
+    out = torch.zeros(9, N, dtype=torch.int16, device="cuda")
+    metro.op_gemm_fp8_experts(o.x, o.xs, 9, None, off, E, 9, W, ws, N, K, 0, out)
+    assert same_bf16(out, o.xv @ o.wv[0].t())
+
+
+def test_norm_and_sums_past_32_bits(metro):
+    rows, d = 5, 512
+    ld = (1 << 32) // 4 + 64
+    x = torch.empty((rows - 1) * ld + d, device="cuda")
+    v = torch.randn(rows, d, device="cuda")
+    for i in range(rows):
+        x[i * ld:i * ld + d] = v[i]
+    gain = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    h, hs, h2, hs2 = (torch.empty(rows, n, dtype=torch.uint8, device="cuda") for n in (d, 4, d, 4))
+    metro.op_rmsnorm_fp8(x, gain, 1e-5, h, hs, rows, d, ldx=ld)
+    metro.op_rmsnorm_fp8(v, gain, 1e-5, h2, hs2, rows, d)
+    assert torch.equal(h, h2) and torch.equal(hs, hs2)
+    y, slot = torch.randn(rows, d, device="cuda").to(torch.bfloat16), torch.arange(rows, dtype=torch.int32, device="cuda")
+    w = torch.ones(rows, device="cuda")
+    metro.op_combine_experts(y, rows, w, slot, rows, 1, d, x, resid=x, ldo=ld)
+    got = torch.stack([x[i * ld:i * ld + d] for i in range(rows)])
+    assert torch.equal(got, v + y.float())
