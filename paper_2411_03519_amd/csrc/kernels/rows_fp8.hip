@@ -12,8 +12,8 @@ namespace metro {
 // ---------------------------------------------------------------------------
 // x' = x + delta;  h = x' * rsqrt(mean(x'^2) + eps) * g;  h to 8-bit rows.
 // One block per row (more rows than blocks: every gridDim-th); a thread holds VPT
-// float4 of it, 32 neighbouring lanes one group of 128.  The norm is fp32 and the codes are rounded from its fp32 values
-// (not from the optional bf16 ones).
+// float4 of it, 32 neighbouring lanes one group of 128.  The norm is fp32 and the
+// codes are rounded from its fp32 values (not from the optional bf16 ones).
 // ---------------------------------------------------------------------------
 template <int NTH, int VPT>
 __global__ __launch_bounds__(NTH) void rmsnorm_fp8_kernel(NormFp8Args a) {
@@ -69,7 +69,8 @@ __global__ __launch_bounds__(NTH) void rmsnorm_fp8_kernel(NormFp8Args a) {
                                    v[j].z * inv * lo_bf16(gw[j].y), v[j].w * inv * hi_bf16(gw[j].y));
       if (a.h16 && i < n4)
         reinterpret_cast<uint2*>(a.h16 + r * a.ldh16)[i] = make_uint2(pack_bf16x2(h.x, h.y), pack_bf16x2(h.z, h.w));
-      float m = fmaxf(fmaxf(fabsf(h.x), fabsf(h.y)), fmaxf(fabsf(h.z), fabsf(h.w)));
+      // (from 0 on: a group of nothing but NaNs has the least power)
+      float m = fmaxf(fmaxf(fmaxf(fabsf(h.x), fabsf(h.y)), fmaxf(fabsf(h.z), fabsf(h.w))), 0.f);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 32));
       const int e = e8m0_of(m);
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(256) void pack_weight_fp8_kernel(const uint16_t* __
     }
     const int k = kb * kGroup + 2 * lane;
     const float a = k < K ? bf16_to_f32(src[row * ld + k]) : 0.f, b = k + 1 < K ? bf16_to_f32(src[row * ld + k + 1]) : 0.f;
-    const int e = e8m0_of(wave_max(fmaxf(fabsf(a), fabsf(b))));
+    const int e = e8m0_of(wave_max(fmaxf(fmaxf(fabsf(a), fabsf(b)), 0.f)));
     const float s = e8m0_inverse(e);
     const uint32_t c = __builtin_amdgcn_cvt_pk_fp8_f32(a * s, b * s, 0, false);
     *reinterpret_cast<uint16_t*>(dst + packed8_offset(row, k, Kp)) = static_cast<uint16_t>(c);

@@ -150,6 +150,20 @@ def test_pack_weight_infinities_and_nans(metro):
     assert byte.tolist() == [119, 247, 247, 119] + [119] * 12
 
 
+def test_groups_of_nothing_but_nans_have_the_least_power(metro):
+    W = np.full((16, 256), 0x7FC0, np.uint16)
+    W[:, :128] = bf16(np.ones((16, 128)))
+    out, scale = filled((16 * 256,)), filled((16 * 4,))
+    metro.op_pack_weight_fp8(dev(W), 256, 16, 256, 256, out, scale)
+    assert (host(out)[2048:] & 0x7F == 0x7F).all() and host(scale).reshape(16, 4)[:, :2].tolist() == [[119, 1]] * 16
+    x = np.ones((2, 200), np.float32)
+    x[1, 7] = np.nan
+    h, hs = filled((2, 256)), filled((2, 4))
+    metro.op_rmsnorm_fp8(dev(x), dev(bf16(np.ones(200))), 0.0, h, hs, 2, 200)
+    assert (host(h)[1, :200] & 0x7F == 0x7F).all() and not host(h)[:, 200:].any()
+    assert host(hs)[:, :2].tolist() == [[119, 119], [1, 1]]
+
+
 # --- norm --------------------------------------------------------------------
 
 
@@ -300,6 +314,28 @@ def test_product_of_nan_rows_stays_in_its_row(metro):
     got, y = bf16_of(out), bf16_bits_to_f64(bf16(o.xv @ o.wv[0].T))
     assert np.isnan(got[11]).all()
     np.testing.assert_array_equal(np.delete(got, 11, 0), np.delete(y, 11, 0))
+
+
+@pytest.mark.parametrize("M,ws", [(5, 0), (40, 0), (40, 8), (150, 0), (700, 0)])
+def test_swiglu_of_nan_and_infinite_rows_stays_in_its_rows(metro, M, ws):
+    N, K = 544, 512
+    o = Operands(7, M, N, K, False)
+    x, xs, F = o.x[0].copy(), o.xs.clone(), N // 2
+    outs = []
+    for bad in (False, True):
+        if bad:
+            x[1, 300] = 0x7F  # a NaN code
+            x[3], xs[3, :4] = 0x7E, 254  # 448 * 2^127 in each column: infinite sums
+        out, scale = filled((M, 384)), filled((M, 4))
+        metro.op_gemm_fp8(dev(x), xs, o.W, o.ws, M, N, K, metro.EPI_FP8_SWIGLU, out, out_scale=scale, workspace=workspace(M, N, ws))
+        outs.append((host(out), host(scale)[:, :3]))
+    (codes, byte), (codes_bad, byte_bad) = outs
+    assert (codes_bad[1, :F] & 0x7F == 0x7F).all() and (byte_bad[1] == 1).all()
+    # infinite where the weights' sum is not next to 0; an infinite factor makes an infinity or a NaN
+    infinite = (np.abs(o.wv[0].sum(1)) > 0.05).reshape(N // 16, 2, 8).any(1).reshape(F)
+    assert infinite.mean() > 0.9 and (codes_bad[3, :F][infinite] & 0x7F == 0x7F).all()
+    for rest in (codes_bad, codes), (byte_bad, byte):
+        np.testing.assert_array_equal(*[np.delete(v, [1, 3], 0) for v in rest])
 
 
 def test_product_repeats_bit_for_bit(metro):
