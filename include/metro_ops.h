@@ -168,7 +168,9 @@ metro_status metro_op_attn_decode_noalloc(const uint16_t* q, const uint16_t* kv,
  * metro_op_combine_experts.
  *
  * All are asynchronous on `stream`, allocate nothing and may be captured into a
- * graph; a workspace belongs to one call at a time. */
+ * graph; a workspace belongs to one call at a time.  Calls of no rows (no tokens,
+ * no slots) do nothing, metro_op_route aside, which writes empty experts; buffers
+ * that would hold no element may be NULL. */
 
 /* Weights of the 8-bit products.  The bf16 matrix W [N, Kp] (as for
  * metro_op_pack_weight: W[n, k] = W_rowmajor[n * ld + k] for k < K, 0 for K <= k <
@@ -185,7 +187,8 @@ metro_status metro_op_pack_weight_fp8(const uint16_t* W_rowmajor, int32_t ld, in
 
 /* Residual addition, RMSNorm and 8-bit rows in one pass over the residual:
  *   x'[r, :] = x[r, :] + delta[r, :]                  (x where delta is NULL)
- *   v[r, :]  = x'[r, :] / sqrt(mean(x'[r, :]^2) + eps) * g       (fp32)
+ *   v[r, :]  = x'[r, :] / sqrt(mean(x'[r, :]^2) + eps) * g
+ * in fp32, the sum of the squares too (a row whose sum passes it has v = 0).
  * h, h_scale <- v as 8-bit rows; h_bf16 <- bf16(v) unless NULL; x_out <- x'
  * unless NULL (x_out only with delta; it may be x).
  *   x, x_out  fp32 [rows, ldx], 16-byte aligned, ldx % 4 == 0

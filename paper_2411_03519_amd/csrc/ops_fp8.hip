@@ -27,7 +27,7 @@ metro_status gemm_fp8(const char* who, metro::GemmFp8Args& a, int32_t epilogue, 
   if (epilogue != metro::kEpi8Bf16 && epilogue != metro::kEpi8SwiGLU)
     return report(METRO_E_INVAL, "%s: epilogue %d (0 or 2)", who, epilogue);
   const bool swiglu = epilogue == metro::kEpi8SwiGLU;
-  if (!a.X || !a.x_scale || !a.W || !a.w_scale || (swiglu ? !a.out8 || !a.out_scale : !a.out16))
+  if (!a.W || !a.w_scale || (a.M > 0 && (!a.X || !a.x_scale || (swiglu ? !a.out8 || !a.out_scale : !a.out16))))
     return report(METRO_E_INVAL, "%s: NULL operand or output", who);
   if (a.M < 0 || a.N <= 0 || a.N % 32 || a.Kp <= 0 || a.Kp % 128)
     return report(METRO_E_INVAL, "%s: bad shape (rows >= 0, N %% 32, Kp %% 128 required)", who);
@@ -67,9 +67,9 @@ metro_status metro_op_rmsnorm_fp8(const float* x, int32_t ldx, const uint16_t* d
                                   float eps, float* x_out, uint16_t* h_bf16, int32_t ldh_bf16, uint8_t* h, int32_t ldh,
                                   uint8_t* h_scale, int32_t lds, int32_t rows, int32_t d, void* stream) {
   clear_error();
-  if (!x || !g || !h || !h_scale || rows < 0 || d <= 0 || d % 4 || d > metro::kNormFp8MaxDim)
+  if (!g || rows < 0 || (rows > 0 && (!x || !h || !h_scale)) || d <= 0 || d % 4 || d > metro::kNormFp8MaxDim)
     return report(METRO_E_INVAL, "rmsnorm_fp8: bad arguments (d %% 4, d <= %d required)", metro::kNormFp8MaxDim);
-  if (x_out && !delta) return report(METRO_E_INVAL, "rmsnorm_fp8: x_out without delta");
+  if (rows > 0 && x_out && !delta) return report(METRO_E_INVAL, "rmsnorm_fp8: x_out without delta");
   if (ldx < d || ldx % 4 || (delta && (ldd < d || ldd % 4)) || (h_bf16 && (ldh_bf16 < d || ldh_bf16 % 4)) ||
       ldh < groups_of(d) * 128 || ldh % 4 || lds < groups_of(d))
     return report(METRO_E_INVAL, "rmsnorm_fp8: row strides must reach d (ldh: d rounded up to 128, lds: its groups) and be "
@@ -96,8 +96,11 @@ metro_status metro_op_gemm_fp8_plan(int32_t M, int32_t N, int32_t Kp, int32_t ep
                                     int32_t* k_slices) {
   clear_error();
   if (!kind || !w_rows || !x_rows || !k_slices || M <= 0 || N <= 0 || N % 32 || Kp <= 0 || Kp % 128 || n_experts < 0 ||
-      M > metro::kGemmFp8MaxRows || n_experts > metro::kGemmFp8MaxExperts || workspace_bytes < 0 || (epilogue != metro::kEpi8Bf16 && epilogue != metro::kEpi8SwiGLU))
+      workspace_bytes < 0 || (epilogue != metro::kEpi8Bf16 && epilogue != metro::kEpi8SwiGLU))
     return report(METRO_E_INVAL, "gemm_fp8_plan: bad shape (N %% 32, Kp %% 128), epilogue or NULL output");
+  if (M > metro::kGemmFp8MaxRows || static_cast<int64_t>(M) * N > metro::kGemmFp8MaxOut ||
+      n_experts > metro::kGemmFp8MaxExperts)
+    return report(METRO_E_INVAL, "gemm_fp8_plan: more than 2^26 rows, 2^36 results or %d experts", metro::kGemmFp8MaxExperts);
   static const int32_t some = 0;
   metro::GemmFp8Args a{};
   a.offsets = n_experts ? &some : nullptr;  // (not read)
@@ -161,7 +164,7 @@ metro_status metro_op_combine_experts(const uint16_t* y, int32_t ldy, int32_t y_
                                       const int32_t* slot, int32_t T, int32_t top_k, int32_t d, const float* resid,
                                       float* out, int32_t ldo, void* stream) {
   clear_error();
-  if (!y || !weights || !slot || !out || T < 0 || y_rows < 0 || top_k <= 0 || d <= 0 || d % 8)
+  if (T < 0 || y_rows < 0 || (T > 0 && (!weights || !slot || !out || (y_rows > 0 && !y))) || top_k <= 0 || d <= 0 || d % 8)
     return report(METRO_E_INVAL, "combine_experts: bad arguments (d %% 8, top_k >= 1 required)");
   if (ldy < d || ldy % 8 || ldo < d || ldo % 4)
     return report(METRO_E_INVAL, "combine_experts: ldy must be a multiple of 8 and ldo one of 4, both from d on");

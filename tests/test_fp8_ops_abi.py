@@ -103,3 +103,27 @@ def test_combine_refusals(lib):
     good = dict(y=BASE, ldy=64, y_rows=10, weights=BASE, slot=BASE, T=5, top_k=2, d=64, resid=BASE, out=BASE, ldo=64, stream=None)
     refused(lib, "metro_op_combine_experts", good, nulls("y", "weights", "slot", "out") + off(8, "y", "resid", "out") +
             [{"T": -1}, {"y_rows": -1}, {"top_k": 0}, {"d": 0}, {"d": 60}, {"ldy": 56}, {"ldy": 68}, {"ldo": 60}, {"ldo": 66}])
+
+
+def test_plan_refusals(lib):
+    v = [ctypes.c_int32() for _ in range(4)]
+
+    def plan(M=100, N=4096, Kp=4096, epilogue=0, n_experts=0, workspace_bytes=0, out=v):
+        return lib.metro_op_gemm_fp8_plan(M, N, Kp, epilogue, n_experts, workspace_bytes, *[None if x is None else ctypes.byref(x) for x in out])
+
+    assert plan() == 0 and plan(M=1 << 24) == 0
+    for bad in (dict(M=0), dict(M=(1 << 26) + 1, N=32), dict(M=(1 << 24) + 1), dict(N=48), dict(Kp=200), dict(epilogue=1),
+                dict(n_experts=-1), dict(n_experts=1025), dict(workspace_bytes=-1), dict(out=v[:3] + [None])):
+        assert plan(**bad) == -1 and b"gemm_fp8_plan" in lib.metro_last_error(), bad
+
+
+def test_calls_without_rows_take_empty_buffers(lib):
+    """Tensors without elements have address 0; nothing is launched for them."""
+    norm = [P(None), 256, P(None), 256, P(BASE), 1e-5, P(None), P(None), 256, P(None), 256, P(None), 4, 0, 256, P(None)]
+    assert lib.metro_op_rmsnorm_fp8(*norm) == 0
+    for epilogue, ldo, ldos in ((0, 320, 0), (2, 256, 2)):
+        tail = [512, 0, 320, epilogue, P(None), P(None), ldo, P(None), ldos, P(None), 0, P(None)]
+        assert lib.metro_op_gemm_fp8(P(None), 512, P(None), 4, P(BASE), P(BASE), *tail) == 0
+        tail[1:3] = [320]
+        assert lib.metro_op_gemm_fp8_experts(P(None), 512, P(None), 4, 0, P(None), P(BASE), 4, 0, P(BASE), P(BASE), *tail) == 0
+    assert lib.metro_op_combine_experts(P(None), 64, 0, P(None), P(None), 0, 2, 64, P(None), P(None), 64, P(None)) == 0
