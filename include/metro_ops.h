@@ -230,10 +230,10 @@ metro_status metro_op_gemm_fp8(const uint8_t* X, int32_t ldx, const uint8_t* x_s
                                float* workspace, int64_t workspace_bytes, void* stream);
 
 /* What metro_op_gemm_fp8 (n_experts 0) or metro_op_gemm_fp8_experts (M slots; X
- * gathered or not, its rows within 4 GiB) would run, for inspection and tests;
- * host only, no device work.  *kind: 0 direct (rows too far apart for the
- * others' 32-bit offsets; never the answer here), 1 streaming, 2 tiled.  *w_rows,
- * *x_rows: rows of W and of X of a workgroup.  *k_slices: slices that a finishing
+ * gathered or not, its rows and their powers within 4 GiB) would run, for
+ * inspection and tests; host only, no device work.  *kind: 0 direct (operands
+ * beyond the others' 32-bit offsets), 1 streaming, 2 tiled.  *w_rows, *x_rows:
+ * rows of W and of X of a workgroup.  *k_slices: slices that a finishing
  * launch sums, 0: none.  Errors: E_INVAL (shape rules of metro_op_gemm_fp8,
  * NULL outputs). */
 metro_status metro_op_gemm_fp8_plan(int32_t M, int32_t N, int32_t Kp, int32_t epilogue, int32_t n_experts,

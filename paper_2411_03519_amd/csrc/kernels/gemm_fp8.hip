@@ -861,10 +861,10 @@ bool passes_caches(const GemmFp8Args& a, const GemmFp8Plan& p) {
 //    few bytes in flight at once: QKV at 25 rows 8.4 against 10.9 of 4 tiled slices,
 //    8B down at 16 rows 15.8 / 17.5, but 70B QKV at 32 rows 26.9 / 23.6.
 GemmFp8Plan plan_gemm_fp8(const GemmFp8Args& a, int epilogue) {
-  // The tiled kernel reaches rows by 32-bit byte offsets from its block's first
-  // element, or from the first row of X where rows are gathered.
+  // The tiled kernel reaches rows and their powers by 32-bit byte offsets from its
+  // block's first row, or from the first row of X where rows are gathered.
   constexpr int64_t kMax = int64_t{1} << 32;
-  const bool fits = static_cast<int64_t>(a.src ? a.x_rows : 256) * a.ldx <= kMax && 256ll * a.Kp <= kMax &&
+  const bool fits = static_cast<int64_t>(a.src ? a.x_rows : 256) * std::max(a.ldx, a.ldxs) <= kMax && 256ll * a.Kp <= kMax &&
                     static_cast<int64_t>(a.N) * (a.Kp / kGroup + 3) <= kMax;
   if (!fits) return {GemmFp8Kind::kDirect, 16, 4, 0, false};
   const bool swiglu = epilogue == kEpi8SwiGLU;

@@ -244,6 +244,23 @@ def test_rows_too_far_apart_for_32_bit_offsets(metro):
         del X
 
 
+@pytest.mark.parametrize("gathered", [False, True])
+def test_powers_too_far_apart_for_32_bit_offsets(metro, gathered):
+    K, N, M, ldxs = 256, 288, 70, 1 << 26  # 4.6 GB from the first row's powers to the last's
+    o = Operands(1, M, N, K, 1, 6)
+    xs = torch.empty((M - 1) * ldxs + 4, dtype=torch.uint8, device="cuda")
+    for i in range(M):
+        xs[i * ldxs:i * ldxs + 4] = o.xs[i]
+    out = torch.zeros(M, N, dtype=torch.int16, device="cuda")
+    if gathered:
+        src = torch.arange(M, dtype=torch.int32, device="cuda")
+        off = torch.tensor([0, M], dtype=torch.int32, device="cuda")
+        metro.op_gemm_fp8_experts(o.x, xs, M, src, off, 1, M, o.W, o.ws, N, K, 0, out, ldxs=ldxs)
+    else:
+        metro.op_gemm_fp8(o.x, xs, o.W, o.ws, M, N, K, 0, out, ldxs=ldxs)
+    assert same_bf16(out, o.xv @ o.wv[0].t())
+
+
 @pytest.mark.parametrize("M,ws", [(20, 0), (70, 8), (200, 0)])
 def test_outputs_past_32_bits(metro, M, ws):
     N, K, ldo = 288, 384, (1 << 32) // M // 16 * 16 + 64  # elements: the last rows lie past 2^32
