@@ -190,6 +190,16 @@ def test_rmsnorm_rows(metro, rows, d, delta, b16):
         assert np.all(np.abs(bf16_of(h16) - v) <= (2.0 ** -8 + SLACK) * np.abs(v))
 
 
+@pytest.mark.parametrize("d", [64, 260, 516, 1028, 2048, 2052, 4100])
+def test_rmsnorm_rows_of_every_number_of_threads(metro, d):
+    rng = np.random.default_rng(d)
+    x, gain = rng.normal(size=(3, d)).astype(np.float32), bf16(1 + 0.1 * rng.normal(size=d))
+    G = -(-d // 128)
+    h, hs = filled((3, 128 * G)), filled((3, -(-G // 4) * 4))
+    metro.op_rmsnorm_fp8(dev(x), dev(gain), 1e-5, h, hs, 3, d)
+    check_rows8(host(h), host(hs)[:, :G], fp8.rms_norm(x, bf16_bits_to_f64(gain), 1e-5))
+
+
 def test_rmsnorm_strides_and_sum_in_place(metro):
     rows, d, ldx, ldd, ldb, ldh, lds = 5, 388, 400, 404, 392, 528, 9
     rng = np.random.default_rng(3)
