@@ -846,8 +846,9 @@ bool passes_caches(const GemmFp8Args& a, const GemmFp8Plan& p) {
 // the times of all plans of 175 products of 1 to 10000 rows (the 8B, 70B and tiny
 // widths, 4 to 32 experts, weights out of the caches); over those the chosen plan
 // is 2% slower than the best one in the mean, 19% at most.  What they say, us:
-//  - a tiled stage (128 columns) costs 0.25 + 0.011 TN TM of a CU, LDS and barriers
-//    first, the matrix cores from TN TM = 48 on, so rows are not rounded up to
+//  - a tiled stage (128 columns) costs 0.25 + 0.011 TN TM of a CU: LDS first (128 x 64
+//    blocks move 72 KiB a stage, 595 clocks; two parts of k in one workgroup or one
+//    barrier a stage change little), the matrix cores from TN TM = 48 on, so rows are not rounded up to
 //    large tiles (8B gate/up at 301 rows as 256 x 256 / 256 x 192 / 256 x 128 tiles
 //    53.6 / 43.2 / 59.6, at 200 rows 48.5 / 43.8 / 37.4), and rounds of 256 workgroups
 //    count whole (8192 rows of 8 experts' down as 256 x 256 / 256 x 192 477 / 438).
