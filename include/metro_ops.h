@@ -212,7 +212,7 @@ metro_status metro_op_rmsnorm_fp8(const float* x, int32_t ldx, const uint16_t* d
  *               aligned, ldx % 16 == 0; x_scale 4-byte aligned, ldxs % 4 == 0,
  *               ldxs >= Kp / 128 rounded up to 4
  *   W, w_scale  as metro_op_pack_weight_fp8 writes them, 16-byte aligned
- * Kp % 128 == 0, N % 32 == 0, M <= 2^26, M * N <= 2^36.  epilogue:
+ * Kp % 128 == 0, N % 32 == 0, M <= 2^26, N <= 2^30, M * N <= 2^36.  epilogue:
  *   0  out_bf16[m*ldo + n] = bf16(acc[m, n]); 8-byte aligned, ldo % 4 == 0, ldo >= N
  *   2  W rows in blocks of 16 = 8 gate rows then the 8 up rows of the same
  *      features (as metro_op_gemm): silu(gate) * up as 8-bit rows of N / 2 values

@@ -71,7 +71,7 @@ enum GemmFp8Epilogue {
 // Dense (offsets null): rows m = 0 .. M-1 of X with one W.  By experts: slots
 // offsets[e] .. offsets[e + 1] - 1 (within 0 .. M) take W + e * N * Kp, slot m
 // row src[m] of X (row m where src is null).
-constexpr int kGemmFp8MaxRows = 1 << 26, kGemmFp8MaxExperts = 1024;
+constexpr int kGemmFp8MaxRows = 1 << 26, kGemmFp8MaxCols = 1 << 30, kGemmFp8MaxExperts = 1024;
 constexpr int64_t kGemmFp8MaxOut = int64_t{1} << 36;  // results: workgroups of any plan that is chosen fit a grid
 struct GemmFp8Args {
   const uint8_t* X;        // [x_rows][ldx] e4m3

@@ -15,6 +15,10 @@ namespace {
 
 bool misaligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
 int32_t groups_of(int32_t k) { return (k + 127) / 128; }
+bool too_large(int32_t M, int32_t N, int32_t experts) {
+  return M > metro::kGemmFp8MaxRows || N > metro::kGemmFp8MaxCols || static_cast<int64_t>(M) * N > metro::kGemmFp8MaxOut ||
+         experts > metro::kGemmFp8MaxExperts;
+}
 
 metro_status launched(hipError_t e, const char* what) {
   if (e == hipSuccess) return METRO_OK;
@@ -31,8 +35,8 @@ metro_status gemm_fp8(const char* who, metro::GemmFp8Args& a, int32_t epilogue, 
     return report(METRO_E_INVAL, "%s: NULL operand or output", who);
   if (a.M < 0 || a.N <= 0 || a.N % 32 || a.Kp <= 0 || a.Kp % 128)
     return report(METRO_E_INVAL, "%s: bad shape (rows >= 0, N %% 32, Kp %% 128 required)", who);
-  if (a.M > metro::kGemmFp8MaxRows || static_cast<int64_t>(a.M) * a.N > metro::kGemmFp8MaxOut || a.E > metro::kGemmFp8MaxExperts)
-    return report(METRO_E_INVAL, "%s: more than 2^26 rows, 2^36 results or %d experts", who, metro::kGemmFp8MaxExperts);
+  if (too_large(a.M, a.N, a.E))
+    return report(METRO_E_INVAL, "%s: more than 2^26 rows, N 2^30, 2^36 results or %d experts", who, metro::kGemmFp8MaxExperts);
   if (a.ldx < a.Kp || a.ldx % 16 || a.ldxs < (groups_of(a.Kp) + 3) / 4 * 4 || a.ldxs % 4)
     return report(METRO_E_INVAL, "%s: ldx must be a multiple of 16 from Kp on, ldxs one of 4 from Kp / 128 on", who);
   if (swiglu ? a.ldo < groups_of(a.N / 2) * 128 || a.ldo % 16 || a.ldos < groups_of(a.N / 2) : a.ldo < a.N || a.ldo % 4)
@@ -98,9 +102,8 @@ metro_status metro_op_gemm_fp8_plan(int32_t M, int32_t N, int32_t Kp, int32_t ep
   if (!kind || !w_rows || !x_rows || !k_slices || M <= 0 || N <= 0 || N % 32 || Kp <= 0 || Kp % 128 || n_experts < 0 ||
       workspace_bytes < 0 || (epilogue != metro::kEpi8Bf16 && epilogue != metro::kEpi8SwiGLU))
     return report(METRO_E_INVAL, "gemm_fp8_plan: bad shape (N %% 32, Kp %% 128), epilogue or NULL output");
-  if (M > metro::kGemmFp8MaxRows || static_cast<int64_t>(M) * N > metro::kGemmFp8MaxOut ||
-      n_experts > metro::kGemmFp8MaxExperts)
-    return report(METRO_E_INVAL, "gemm_fp8_plan: more than 2^26 rows, 2^36 results or %d experts", metro::kGemmFp8MaxExperts);
+  if (too_large(M, N, n_experts))
+    return report(METRO_E_INVAL, "gemm_fp8_plan: more than 2^26 rows, N 2^30, 2^36 results or %d experts", metro::kGemmFp8MaxExperts);
   static const int32_t some = 0;
   metro::GemmFp8Args a{};
   a.offsets = n_experts ? &some : nullptr;  // (not read)

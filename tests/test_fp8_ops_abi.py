@@ -127,3 +127,11 @@ def test_calls_without_rows_take_empty_buffers(lib):
         tail[1:3] = [320]
         assert lib.metro_op_gemm_fp8_experts(P(None), 512, P(None), 4, 0, P(None), P(BASE), 4, 0, P(BASE), P(BASE), *tail) == 0
     assert lib.metro_op_combine_experts(P(None), 64, 0, P(None), P(None), 0, 2, 64, P(None), P(None), 64, P(None)) == 0
+
+
+def test_widths_past_2_to_30_are_refused(lib):
+    for change in ({"M": 1, "N": (1 << 30) + 32, "ldo": (1 << 30) + 32}, {"M": 1, "N": (1 << 31) - 32, "ldo": (1 << 31) - 4}):
+        refused(lib, "metro_op_gemm_fp8", GEMM, [change], b"2^30")
+    v = [ctypes.c_int32() for _ in range(4)]
+    assert lib.metro_op_gemm_fp8_plan(1, (1 << 31) - 32, 128, 0, 0, 0, *[ctypes.byref(x) for x in v]) == -1
+    assert lib.metro_op_gemm_fp8_plan(1, 1 << 30, 128, 0, 0, 0, *[ctypes.byref(x) for x in v]) == 0
