@@ -8,12 +8,10 @@
 // experts comes first must not hang on the rounding of an exponential.
 //
 // Bytes are few (31527 tokens of 128 experts: 20 MB, 4 us at the rate of a copy), and
-// the vector ALU bounds it: 535 instructions a token there, 43 us in all. Of the
-// choices' 34.6 the k largest take 10, the groups 8, the exponentials 5.5, the
-// stores 2; the scan and the places another 8 of launches.  A wave of 64 lanes has
-// one token of more than 32 experts (32 lanes of 4 experts each: 33.9, 16 of 8 the
-// same).  Up to 64 tokens one workgroup does everything in one launch, 3.4 us for
-// 25, since a second launch costs as much again.
+// the vector ALU bounds it: 25 us there for the choices, in which the k largest, the
+// groups and the exponentials have about equal parts, and 5 each for the scan and the
+// places, mostly launches.  Up to 64 tokens one workgroup does everything in one
+// launch, 3.5 us for 25 tokens of 8 experts, since a second launch costs as much again.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -131,90 +129,93 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, const float (&z)
     c[q] = e < a.E ? choosable(s[q] + (a.bias ? static_cast<double>(a.bias[e]) : 0.0)) : kNone;
   }
   if (a.groups > 1) {
-    // `parts` neighbouring lanes to a group, each with every parts-th expert
+    // `parts` neighbouring lanes to a group, each with every parts-th expert; where
+    // the groups outnumber the lanes, the lanes take them in turn
     const int per = a.E / a.groups;
     int parts = 1;
     while (2 * parts * a.groups <= LPT) parts *= 2;
-    const int g = l / parts, part = l % parts;
+    const int part = l % parts, step = LPT / parts;
     double* const best = room + a.E;
     wave_fence();
 #pragma unroll
     for (int q = 0; q < EPL; ++q)
       if (q * LPT + l < a.E) room[q * LPT + l] = c[q];
     wave_fence();
-    double first = -__builtin_inf(), second = first;
-    if (g < a.groups)
-      for (int i = part; i < per; i += parts) {
-        const double v = room[g * per + i];
-        second = fmax(second, fmin(first, v));
-        first = fmax(first, v);
+    for (int g0 = 0; g0 < a.groups; g0 += step) {
+      const int g = g0 + l / parts;
+      double first = -__builtin_inf(), second = first;
+      if (g < a.groups)
+        for (int i = part; i < per; i += parts) {
+          const double v = room[g * per + i];
+          second = fmax(second, fmin(first, v));
+          first = fmax(first, v);
+        }
+      for (int o = 1; o < parts; o *= 2) {
+        const double f = __shfl_xor(first, o), h = __shfl_xor(second, o);
+        second = fmax(fmin(first, f), fmax(second, h));
+        first = fmax(first, f);
       }
-    for (int o = 1; o < parts; o *= 2) {
-      const double f = __shfl_xor(first, o), h = __shfl_xor(second, o);
-      second = fmax(fmin(first, f), fmax(second, h));
-      first = fmax(first, f);
+      if (g < a.groups && part == 0) best[g] = choosable(per > 1 ? first + second : first);
     }
-    const double mine = choosable(per > 1 ? first + second : first);
-    if (g < a.groups && part == 0) best[g] = mine;
     wave_fence();
-    int ahead = 0;
-    if (g < a.groups)
-      for (int i = part; i < a.groups; i += parts) ahead += best[i] > mine || (best[i] == mine && i < g);
-    for (int o = 1; o < parts; o *= 2) ahead += __shfl_xor(ahead, o);
-    wave_fence();
-    if (g < a.groups && part == 0) best[g] = ahead < a.top_groups ? 1.0 : 0.0;
+    for (int g0 = 0; g0 < a.groups; g0 += step) {
+      const int g = g0 + l / parts;
+      int ahead = 0;
+      if (g < a.groups) {
+        const double mine = best[g];
+        for (int i = part; i < a.groups; i += parts) ahead += best[i] > mine || (best[i] == mine && i < g);
+      }
+      for (int o = 1; o < parts; o *= 2) ahead += __shfl_xor(ahead, o);
+      // (in the place of the choices, which are read)
+      if (g < a.groups && part == 0) room[g] = ahead < a.top_groups ? 1.0 : 0.0;
+    }
     wave_fence();
 #pragma unroll
     for (int q = 0; q < EPL; ++q) {
       const int e = q * LPT + l;
-      if (e < a.E && best[e / per] == 0.0) c[q] = kNone;
+      if (e < a.E && room[e / per] == 0.0) c[q] = kNone;
     }
   }
   // The k largest, one after another.  A choice's upper 32 bits, as an integer of
   // the same order, mostly tell the largest alone; where two share them (in any
   // token of the wave) the doubles decide, and their ties the lowest index.
-  // (31527 tokens over 128 experts, 8 chosen: doubles alone 49.5 us, so 41.8.)
   uint32_t key[EPL];
 #pragma unroll
   for (int q = 0; q < EPL; ++q) {
     const uint32_t hi = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, c[q]) >> 32);
     key[q] = c[q] != c[q] ? 0u : hi ^ ((hi >> 31) ? 0xffffffffu : 0x80000000u);
   }
-  auto lanes_of = [&](bool p) -> uint64_t {
-    if constexpr (LPT == 64) return __ballot(p);  // (scalar from here on)
-    return (__ballot(p) >> ((threadIdx.x & 63) / LPT * LPT)) & (~0ull >> (64 - LPT));
-  };
   for (int j = 0; j < a.k; ++j) {
     uint32_t top = key[0];
 #pragma unroll
     for (int q = 1; q < EPL; ++q) top = max(top, key[q]);
     top = lanes_max<LPT>(top);
-    uint64_t bits[EPL];
+    bool best[EPL];
     int sharing = 0;
 #pragma unroll
     for (int q = 0; q < EPL; ++q) {
-      bits[q] = lanes_of(key[q] == top);
-      sharing += __popcll(bits[q]);
+      best[q] = key[q] == top;
+      sharing += __popcll(__ballot(best[q]));
     }
-    if (LPT == 64 ? sharing > 1 : __any(sharing > 1)) {
-      double m = c[0];
+    if (sharing != kWave / LPT) {  // more than one in some token
+      double m = kNone;
 #pragma unroll
-      for (int q = 1; q < EPL; ++q) m = fmax(m, c[q]);
+      for (int q = 0; q < EPL; ++q) m = fmax(m, key[q] ? c[q] : kNone);
       m = lanes_reduce<LPT>(m, mx);
+      bool found = false;
 #pragma unroll
-      for (int q = 0; q < EPL; ++q) bits[q] = lanes_of(c[q] == m);
+      for (int q = 0; q < EPL; ++q) {
+        const bool tie = key[q] && c[q] == m;
+        uint64_t bits = __ballot(tie);
+        if constexpr (LPT < 64) bits = (bits >> ((threadIdx.x & 63) / LPT * LPT)) & (~0ull >> (64 - LPT));
+        best[q] = tie && !found && l == __builtin_ctzll(bits);
+        found = found || bits;
+      }
     }
-    bool found = false;
 #pragma unroll
     for (int q = 0; q < EPL; ++q) {
-      if (!found && bits[q]) {
-        found = true;
-        if (l == __builtin_ctzll(bits[q])) {
-          place[q] = j;
-          c[q] = kNone;
-          key[q] = 0;
-        }
-      }
+      place[q] = best[q] ? j : place[q];
+      key[q] = best[q] ? 0u : key[q];
     }
   }
   double sum = 0.0;
@@ -262,11 +263,13 @@ __device__ __forceinline__ void prefix(int32_t* v, int n, int32_t* wave_sums) {
   __syncthreads();
 }
 
+constexpr int kRouteThreads = 512;
+
 // Choices of kRouteBlock tokens.  ALONE: they are all there are, and the block
 // finds their places too; else it leaves its count of each expert in ws.
-// (waves per SIMD: two workgroups of 1024 threads have to fit a CU)
-template <int NTH, int LPT, int EPL, bool ALONE>
-__global__ __launch_bounds__(NTH, NTH == 1024 && EPL <= 2 ? 8 : 4) void route_kernel(RouteArgs a) {
+template <int LPT, int EPL, bool ALONE>
+__global__ __launch_bounds__(kRouteThreads, 4) void route_kernel(RouteArgs a) {
+  constexpr int NTH = kRouteThreads;
   extern __shared__ double room[];
   __shared__ unsigned long long mask[kRouteMaxExperts];
   __shared__ int32_t base[kRouteMaxExperts + 1], wave_sums[NTH / 64];
@@ -383,24 +386,39 @@ __global__ __launch_bounds__(256) void route_place_kernel(RouteArgs a, int nb) {
   }
 }
 
-template <int NTH, bool ALONE>
+// Lanes of a token and experts of a lane.  Up to 8 experts a lane keep most
+// instructions busy for several tokens at once (31527 tokens of 128 experts, 8 of them
+// chosen in 4 of 8 groups, 16 x 8 / 32 x 4 / 64 x 2: 25.0 / 28.1 / 38.4 us; of 256, 32 x 8 / 64 x 4
+// 46.4 / 55.8; of 64, 16 x 4 / 32 x 2 15.6 / 19.9; 8 x 8 14.9, whose room would not fit);
+// where every token has a wave of its own, more lanes are sooner done (one token
+// of 64 experts 64 x 1 / 16 x 4 4.3 / 6.1, of 256 64 x 4 / 32 x 8 7.4 / 10.3).  (1024 threads: 25.6 and
+// 29.0 for 16 x 8 and 32 x 4; 256: 32.4 and 37.7.)
+template <bool ALONE>
 void launch_choices(const RouteArgs& a, int nb, hipStream_t s) {
   auto go = [&](auto lpt, auto epl) {
     constexpr int LPT = decltype(lpt)::value, EPL = decltype(epl)::value;
-    const uint32_t room = a.groups > 1 ? static_cast<uint32_t>(NTH / LPT * (a.E + a.groups) * sizeof(double)) : 0;
-    route_kernel<NTH, LPT, EPL, ALONE><<<dim3(nb), dim3(NTH), room, s>>>(a);
+    // experts and groups (no more than experts) of the tokens at a time, beside the masks and bases
+    static_assert(kRouteThreads / LPT * (LPT * EPL + std::min(LPT * EPL, kRouteMaxGroups)) * sizeof(double) <= 56 * 1024);
+    const uint32_t room = a.groups > 1 ? static_cast<uint32_t>(kRouteThreads / LPT * (a.E + a.groups) * sizeof(double)) : 0;
+    route_kernel<LPT, EPL, ALONE><<<dim3(nb), dim3(kRouteThreads), room, s>>>(a);
   };
   using std::integral_constant;
-  constexpr bool kFew = ALONE || NTH == 1024, kMany = NTH == 512;  // up to 256 experts; more
-  if constexpr (kFew) {
-    if (a.E <= 8) return go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
-    if (a.E <= 16) return go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
-    if (a.E <= 32) return go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
-    if (a.E <= 64) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-    if (a.E <= 128) return go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-    if (a.E <= 256) return go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  if constexpr (ALONE) {
+    if (a.T <= kRouteThreads / 64 && a.E > 8 && a.E <= 256) {
+      if (a.E <= 16) return go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+      if (a.E <= 32) return go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+      if (a.E <= 64) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+      if (a.E <= 128) return go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+      return go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    }
   }
-  if constexpr (kMany) go(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  if (a.E <= 8) return go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+  if (a.E <= 16) return go(integral_constant<int, 8>{}, integral_constant<int, 2>{});
+  if (a.E <= 32) return go(integral_constant<int, 8>{}, integral_constant<int, 4>{});
+  if (a.E <= 64) return go(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+  if (a.E <= 128) return go(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+  if (a.E <= 256) return go(integral_constant<int, 32>{}, integral_constant<int, 8>{});
+  go(integral_constant<int, 64>{}, integral_constant<int, 8>{});
 }
 
 }  // namespace
@@ -411,13 +429,10 @@ constexpr int kRouteOwnSums = 32;
 hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
   const int nb = (a.T + kRouteBlock - 1) / kRouteBlock;
   if (nb <= 1) {
-    launch_choices<512, true>(a, 1, s);
+    launch_choices<true>(a, 1, s);
     return hipGetLastError();
   }
-  if (a.E <= 256)
-    launch_choices<1024, false>(a, nb, s);
-  else
-    launch_choices<512, false>(a, nb, s);  // (room of 512 experts for 16 tokens at a time would pass 64 KiB)
+  launch_choices<false>(a, nb, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (nb <= kRouteOwnSums) {

@@ -404,6 +404,16 @@ def test_route_ties_go_to_the_lowest_index(metro):
     check_route(metro, z, 5, scoring=1, n_groups=8, top_groups=2)
 
 
+@pytest.mark.parametrize("T", [3, 9, 64, 150])
+@pytest.mark.parametrize("E,k,groups,top", [(16, 2, 16, 5), (24, 3, 12, 4), (32, 6, 32, 7), (48, 5, 24, 9), (64, 6, 32, 5), (128, 8, 64, 20),
+                                            (130, 8, 26, 3), (256, 8, 64, 6), (512, 9, 64, 9)])
+def test_route_more_groups_than_lanes_and_equal_scores(metro, T, E, k, groups, top):
+    rng = np.random.default_rng([T, E, groups])
+    check_route(metro, rng.integers(0, 4, (T, E)) / 2.0, k, None, T % 2, groups, top)
+    z = rng.integers(0, 2, (T, E)) + 2.0 ** -22 * rng.integers(0, 3, (T, E))  # mostly apart in the lower bits alone
+    check_route(metro, z, k, None, 1 - T % 2, groups, top)
+
+
 @pytest.mark.parametrize("T", [5, 70])
 @pytest.mark.parametrize("scoring", [0, 1])
 def test_route_masked_infinite_and_nan_logits(metro, T, scoring):
