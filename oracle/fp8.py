@@ -115,7 +115,7 @@ def route(logits, k: int, bias=None, sigmoid=False, groups=1, top_groups=1, reno
         experts[t] = sorted(left, key=lambda e: (-c[e], e))[:k]
         total = sum(s[e] for e in experts[t])
         for j, e in enumerate(experts[t]):
-            weights[t, j] = s[e] * scale / (total if renormalise and total != 0 else 1.0)
+            weights[t, j] = s[e] / (total if renormalise and total != 0 else 1.0) * scale
     offsets, src, slot = [0], [], np.zeros((T, k), np.int64)
     for e in range(E):
         for t in range(T):

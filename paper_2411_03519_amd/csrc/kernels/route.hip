@@ -223,13 +223,16 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, const float (&z)
   for (int q = 0; q < EPL; ++q)
     if (place[q] >= 0) sum += s[q];
   sum = lanes_reduce<LPT>(sum, add);
-  const double by = a.renormalise && sum != 0.0 ? a.scale / sum : a.scale;
+  const bool over_sum = a.renormalise && sum != 0.0;
+  // scale / sum is infinite for the least of sums: there both sides are taken 2^800 larger, which is exact
+  const double up = over_sum && sum < 0x1p-800 ? 0x1p800 : 1.0;
+  const double by = over_sum ? a.scale / (sum * up) : a.scale;
 #pragma unroll
   for (int q = 0; q < EPL; ++q)
     if (valid && place[q] >= 0) {
       const int e = q * LPT + l;
       a.experts[t * a.k + place[q]] = e;
-      a.weights[t * a.k + place[q]] = static_cast<float>(s[q] * by);
+      a.weights[t * a.k + place[q]] = static_cast<float>(s[q] * up * by);
       atomicOr(&mask[e], 1ull << bit);
     }
 }
