@@ -243,8 +243,9 @@ metro_status metro_op_gemm_fp8_plan(int32_t M, int32_t N, int32_t Kp, int32_t ep
 /* Routing of T tokens to top_k of n_experts experts each.  With z = logits[t, :]
  * and, in fp64, s = softmax(z) (scoring 0) or 1 / (1 + exp(-z)) (scoring 1):
  *   choice c = s + bias (bias fp32 [n_experts] or NULL; -inf shuts an expert out)
- *   experts in n_groups equal runs; a group's score is the sum of its two
- *   largest c (its one c where it has one expert); the top_groups best groups stay
+ *   experts in n_groups equal runs; a group's score is the sum of its two largest
+ *   c among the open experts (its one c where one is open, behind every other
+ *   group where none is); the top_groups best groups stay
  *   experts[t, :]  the top_k largest c of theirs, largest first
  *   weights[t, :]  their s * scale, with renormalise s / sum of the top_k s * scale
  *                  (0 where that sum is 0)

@@ -108,8 +108,8 @@ def route(logits, k: int, bias=None, sigmoid=False, groups=1, top_groups=1, reno
         c = [v if v == v else -math.inf for v in c]
         best = []
         for g in range(groups):
-            two = sorted(c[g * per:(g + 1) * per], reverse=True)[:2]
-            best.append(sum(two) if sum(two) == sum(two) else -math.inf)
+            open_ = sorted(v for v in c[g * per:(g + 1) * per] if v > -math.inf)
+            best.append(sum(open_[-2:]) if open_ else -math.inf)
         kept = sorted(range(groups), key=lambda g: (-best[g], g))[:top_groups]
         left = [e for e in range(E) if e // per in kept]
         experts[t] = sorted(left, key=lambda e: (-c[e], e))[:k]

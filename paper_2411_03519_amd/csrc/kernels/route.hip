@@ -2,7 +2,7 @@
 // and the places of the tokens' rows in the experts' order.
 //
 // s = softmax or sigmoid of a token's logits, c = s + bias; of `groups` equal
-// runs of experts the top_groups with the largest sum of their two best c stay;
+// runs of experts the top_groups with the largest sum of their two best open c stay;
 // of their experts the k largest c are chosen, ties to the lowest index; weights
 // are their s (over their sum).  Scores are computed in fp64: which of two
 // experts comes first must not hang on the rounding of an exponential.
@@ -155,7 +155,8 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, const float (&z)
         second = fmax(fmin(first, f), fmax(second, h));
         first = fmax(first, f);
       }
-      if (g < a.groups && part == 0) best[g] = choosable(per > 1 ? first + second : first);
+      // (an expert that is shut out adds nothing, and does not shut out its group)
+      if (g < a.groups && part == 0) best[g] = second == -__builtin_inf() ? first : first + second;
     }
     wave_fence();
     for (int g0 = 0; g0 < a.groups; g0 += step) {

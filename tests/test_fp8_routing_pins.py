@@ -7,6 +7,21 @@ from oracle import fp8
 INF = float("inf")
 
 
+def test_shut_out_experts_leave_their_group_to_the_open_ones():
+    z = [[5.0, 4.0, 0.0, 3.0]]
+    experts, w, offsets, src, slot = fp8.route(z, 1, [-INF, -INF, 0, -INF], groups=2)
+    assert experts.tolist() == [[2]] and w.tolist() == [[1.0]] and offsets.tolist() == [0, 0, 0, 1, 1]
+    # groups {0, 1, 2}, {3, 4, 5} of sigmoids: one open expert of 0.9 against two of 0.3, then against two of 0.6
+    s = np.array([[0.9, 0.5, 0.5, 0.3, 0.3, 0.5], [0.9, 0.5, 0.5, 0.6, 0.6, 0.5]])
+    experts, *_ = fp8.route(np.log(s / (1 - s)), 1, [0, -INF, -INF, 0, 0, -INF], sigmoid=True, groups=2)
+    assert experts.tolist() == [[0], [3]]
+
+
+def test_a_wanted_expert_beside_a_shut_out_one():
+    experts, *_ = fp8.route([[5.0, 4.0, 0.0, 3.0]], 1, [0, 0, INF, -INF], groups=2)
+    assert experts.tolist() == [[2]]
+
+
 def test_weights_of_scores_next_to_nothing():
     want = 1 / (1 + np.exp(-0.5))
     for below in (650, 700, 709, 712):

@@ -48,3 +48,36 @@ def test_route_sigmoids_next_to_nothing(metro, T, scale, below):
     z = np.tile([-below, -below - 0.125, -900, -900], (T, 1))
     got = check_small(metro, z, 2, None, 1, scale)
     np.testing.assert_allclose(got[1].sum(1), 0.0 if below > 709.8 else scale, rtol=2.0 ** -22)
+
+
+# --- shut out experts ---------------------------------------------------------------
+
+
+@pytest.mark.parametrize("T", [1, 8, 64, 65, 200, 2100])
+@pytest.mark.parametrize("scoring", [0, 1])
+@pytest.mark.parametrize("E,k,groups,top", [(4, 1, 2, 1), (8, 2, 2, 1), (8, 2, 4, 2), (8, 4, 1, 1), (16, 3, 16, 4), (32, 4, 8, 3), (64, 6, 32, 5),
+                                            (128, 8, 8, 4), (256, 8, 64, 6), (512, 9, 8, 2)])
+def test_route_shut_out_experts(metro, T, scoring, E, k, groups, top):
+    """Of every group none to two are left open, of some runs of groups nothing."""
+    rng = np.random.default_rng([T, E, groups, scoring])
+    z, per = rng.normal(size=(T, E)) * 2, E // groups
+    for open_ in (0, 1, 2):
+        bias = np.full(E, -np.inf, np.float32)
+        for g in range(groups):
+            n = min(per, int(rng.integers(0, open_ + 1)))
+            bias[g * per + rng.permutation(per)[:n]] = rng.normal(size=n) * 0.1
+        got = check_route(metro, z, k, bias, scoring, groups, top, renormalise=open_ != 1, scale=1.5)
+        shut = np.isneginf(bias)[got[0]]
+        # where the experts left are enough, none that is shut out is chosen
+        if groups == 1 or top == groups:
+            assert shut.sum(1).tolist() == [max(0, k - int(np.isfinite(bias).sum()))] * T
+
+
+@pytest.mark.parametrize("T", [3, 70])
+def test_route_keeps_the_group_of_the_only_open_expert(metro, T):
+    z = np.tile([5.0, 4, 0, 3], (T, 1))
+    got = check_route(metro, z, 1, [-np.inf, -np.inf, 0, -np.inf], n_groups=2, top_groups=1)
+    assert (got[0] == 2).all() and (got[1] == 1).all()
+    # a wanted expert beside a shut out one
+    got = check_route(metro, z, 1, [0, 0, np.inf, -np.inf], n_groups=2, top_groups=1)
+    assert (got[0] == 2).all()
