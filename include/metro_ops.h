@@ -249,10 +249,11 @@ metro_status metro_op_gemm_fp8_plan(int32_t M, int32_t N, int32_t Kp, int32_t ep
  *   experts[t, :]  the top_k largest c of theirs, largest first
  *   weights[t, :]  their s * scale, with renormalise s / sum of the top_k s * scale
  *                  (0 where that sum is 0)
- * Ties go to the lowest index.  A NaN choice comes behind every number: where too
- * few numbers are left, the lowest indices of the staying groups are chosen, so
- * indices are always distinct and in range.  A row of -inf has s = 0; a NaN or
- * +inf in a softmax row makes its weights NaN.
+ * Ties go to the lowest index.  A NaN choice counts as -inf: where too few open
+ * experts are left, the lowest indices of the staying groups are chosen, so
+ * indices are always distinct and in range.  An expert that its bias shuts out
+ * has s = 0 among the weights then.  A row of -inf has s = 0; a NaN or +inf in a
+ * softmax row makes its weights NaN (those of shut out experts may stay 0).
  * And the experts' order of the T * top_k rows, tokens ascending within an expert:
  *   offsets [n_experts + 1]: expert e has slots offsets[e] .. offsets[e + 1] - 1
  *   src  [T * top_k]: token of a slot;  slot [T, top_k]: slot of a choice

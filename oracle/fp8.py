@@ -113,9 +113,10 @@ def route(logits, k: int, bias=None, sigmoid=False, groups=1, top_groups=1, reno
         kept = sorted(range(groups), key=lambda g: (-best[g], g))[:top_groups]
         left = [e for e in range(E) if e // per in kept]
         experts[t] = sorted(left, key=lambda e: (-c[e], e))[:k]
-        total = sum(s[e] for e in experts[t])
+        shut = [bias is not None and bias[e] == -math.inf for e in range(E)]
+        total = sum(s[e] for e in experts[t] if not shut[e])
         for j, e in enumerate(experts[t]):
-            weights[t, j] = s[e] / (total if renormalise and total != 0 else 1.0) * scale
+            weights[t, j] = (0.0 if shut[e] else s[e]) / (total if renormalise and total != 0 else 1.0) * scale
     offsets, src, slot = [0], [], np.zeros((T, k), np.int64)
     for e in range(E):
         for t in range(T):

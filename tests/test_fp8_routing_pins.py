@@ -22,6 +22,19 @@ def test_a_wanted_expert_beside_a_shut_out_one():
     assert experts.tolist() == [[2]]
 
 
+def test_shut_out_experts_that_fill_up_have_no_weight():
+    z = np.log([[1.0, 2, 3, 4]])
+    for renormalise, first in ((True, 2.0), (False, 0.6)):
+        experts, w, *_ = fp8.route(z, 3, [-INF, -INF, 0, -INF], renormalise=renormalise, scale=2.0)
+        assert experts.tolist() == [[2, 0, 1]]
+        np.testing.assert_allclose(w, [[first, 0, 0]], rtol=1e-15)
+    experts, w, *_ = fp8.route(z, 2, [-INF] * 4, groups=2)
+    assert experts.tolist() == [[0, 1]] and w.tolist() == [[0, 0]]
+    # not even where the score is a NaN
+    experts, w, *_ = fp8.route([[np.nan, 1.0]], 2, [-INF, 0], sigmoid=True)
+    assert experts.tolist() == [[1, 0]] and w.tolist() == [[1, 0]]
+
+
 def test_weights_of_scores_next_to_nothing():
     want = 1 / (1 + np.exp(-0.5))
     for below in (650, 700, 709, 712):

@@ -68,6 +68,7 @@ def test_route_shut_out_experts(metro, T, scoring, E, k, groups, top):
             bias[g * per + rng.permutation(per)[:n]] = rng.normal(size=n) * 0.1
         got = check_route(metro, z, k, bias, scoring, groups, top, renormalise=open_ != 1, scale=1.5)
         shut = np.isneginf(bias)[got[0]]
+        assert not got[1][shut].any()
         # where the experts left are enough, none that is shut out is chosen
         if groups == 1 or top == groups:
             assert shut.sum(1).tolist() == [max(0, k - int(np.isfinite(bias).sum()))] * T
@@ -78,6 +79,18 @@ def test_route_keeps_the_group_of_the_only_open_expert(metro, T):
     z = np.tile([5.0, 4, 0, 3], (T, 1))
     got = check_route(metro, z, 1, [-np.inf, -np.inf, 0, -np.inf], n_groups=2, top_groups=1)
     assert (got[0] == 2).all() and (got[1] == 1).all()
+    got = check_route(metro, z, 2, [-np.inf, -np.inf, 0, -np.inf])
+    assert (got[0] == [2, 0]).all() and (got[1] == [1, 0]).all()
     # a wanted expert beside a shut out one
     got = check_route(metro, z, 1, [0, 0, np.inf, -np.inf], n_groups=2, top_groups=1)
     assert (got[0] == 2).all()
+
+
+@pytest.mark.parametrize("T", [3, 70])
+@pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
+def test_route_shut_out_experts_of_any_logit_have_no_weight(metro, T, value):
+    z = np.tile([value, 1.0, value, 2.0], (T, 1))
+    with np.errstate(all="ignore"):
+        got = check_route(metro, z, 4, [-np.inf, 0, -np.inf, 0], scoring=1, scale=2.0)
+        assert (got[0] == [3, 1, 0, 2]).all() and (got[1][:, 2:] == 0).all()
+        check_route(metro, z, 4, [-np.inf, 0, -np.inf, 0], scoring=1, renormalise=False)
