@@ -217,7 +217,8 @@ metro_status metro_op_rmsnorm_fp8(const float* x, int32_t ldx, const uint16_t* d
  *   2  W rows in blocks of 16 = 8 gate rows then the 8 up rows of the same
  *      features (as metro_op_gemm): silu(gate) * up as 8-bit rows of N / 2 values
  *      in out_fp8 [M, ldo] (16-byte aligned, ldo % 16 == 0, ldo >= N / 2 rounded up
- *      to 128) and out_scale [M, ldos] (ldos >= ceil(N / 256)), rounded from fp32
+ *      to 128) and out_scale [M, ldos] (ldos >= ceil(N / 256)), rounded from fp32;
+ *      silu(gate) is 0 for gates below -87.33, whose sigmoid is below 2^-126
  * The other output is NULL.
  * workspace: NULL, or device fp32 of workspace_bytes, 16-byte aligned: small
  * products may then run as k slices (ks * M * N floats for ks <= 8 slices where
