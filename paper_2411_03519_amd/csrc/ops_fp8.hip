@@ -136,7 +136,8 @@ metro_status metro_op_route(const float* logits, int32_t ldl, const float* bias,
     return report(METRO_E_INVAL, "route: top_k must be 1 .. %d and at most the experts of top_groups groups",
                   metro::kRouteMaxTopK);
   if (T > metro::kRouteMaxTokens) return report(METRO_E_INVAL, "route: more than %d tokens", metro::kRouteMaxTokens);
-  if (misaligned(logits, 4) || misaligned(bias, 4) || misaligned(weights, 4) || misaligned(workspace, 4))
+  if (misaligned(logits, 4) || misaligned(bias, 4) || misaligned(experts, 4) || misaligned(weights, 4) ||
+      misaligned(offsets, 4) || misaligned(src, 4) || misaligned(slot, 4) || misaligned(workspace, 4))
     return report(METRO_E_INVAL, "route: misaligned buffer");
   if (T > metro::kRouteBlock) {
     const int64_t need = 4ll * n_experts * ((T + metro::kRouteBlock - 1) / metro::kRouteBlock);
@@ -156,6 +157,8 @@ metro_status metro_op_gemm_fp8_experts(const uint8_t* X, int32_t ldx, const uint
                                        void* stream) {
   clear_error();
   if (!offsets || n_experts <= 0) return report(METRO_E_INVAL, "gemm_fp8_experts: NULL offsets or n_experts <= 0");
+  if (misaligned(src, 4) || misaligned(offsets, 4))
+    return report(METRO_E_INVAL, "gemm_fp8_experts: src and offsets must be 4-byte aligned");
   if (x_rows < 0 || (src ? R > 0 && x_rows < 1 : x_rows < R))
     return report(METRO_E_INVAL, "gemm_fp8_experts: x_rows must cover the slots (without src) or be at least 1");
   metro::GemmFp8Args a{X, x_scale, W, w_scale, src, offsets, out_bf16, out_fp8, out_scale, nullptr, 0,
