@@ -241,6 +241,12 @@ metro_status metro_op_gemm_fp8_plan(int32_t M, int32_t N, int32_t Kp, int32_t ep
                                     int64_t workspace_bytes, int32_t* kind, int32_t* w_rows, int32_t* x_rows,
                                     int32_t* k_slices);
 
+/* Whether that product's weights would pass the caches by (*w_bypass 1, else 0):
+ * such kernels are built apart, so tests of every variant need to tell them.
+ * Host only; arguments and errors as metro_op_gemm_fp8_plan. */
+metro_status metro_op_gemm_fp8_plan_bypass(int32_t M, int32_t N, int32_t Kp, int32_t epilogue, int32_t n_experts,
+                                           int64_t workspace_bytes, int32_t* w_bypass);
+
 /* Routing of T tokens to top_k of n_experts experts each.  With z = logits[t, :]
  * and, in fp64, s = softmax(z) (scoring 0) or 1 / (1 + exp(-z)) (scoring 1):
  *   choice c = s + bias (bias fp32 [n_experts] or NULL; -inf shuts an expert out)

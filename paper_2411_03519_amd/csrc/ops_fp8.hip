@@ -51,6 +51,24 @@ metro_status gemm_fp8(const char* who, metro::GemmFp8Args& a, int32_t epilogue, 
   return launched(metro::launch_gemm_fp8(a, epilogue, static_cast<hipStream_t>(stream)), who);
 }
 
+// the plan of a product that is described by its sizes alone
+metro_status plan_of(const char* who, int32_t M, int32_t N, int32_t Kp, int32_t epilogue, int32_t n_experts,
+                     int64_t workspace_bytes, bool outputs, metro::GemmFp8Plan& p) {
+  if (!outputs || M <= 0 || N <= 0 || N % 32 || Kp <= 0 || Kp % 128 || n_experts < 0 || workspace_bytes < 0 ||
+      (epilogue != metro::kEpi8Bf16 && epilogue != metro::kEpi8SwiGLU))
+    return report(METRO_E_INVAL, "%s: bad shape (N %% 32, Kp %% 128), epilogue or NULL output", who);
+  if (too_large(M, N, n_experts))
+    return report(METRO_E_INVAL, "%s: more than 2^26 rows, N 2^30, 2^36 results or %d experts", who, metro::kGemmFp8MaxExperts);
+  static const int32_t some = 0;
+  metro::GemmFp8Args a{};
+  a.offsets = n_experts ? &some : nullptr;  // (not read)
+  a.E = n_experts ? n_experts : 1;
+  a.M = M, a.N = N, a.Kp = a.ldx = Kp;
+  a.ws_floats = workspace_bytes / 4;
+  p = metro::plan_gemm_fp8(a, epilogue);
+  return METRO_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -99,24 +117,26 @@ metro_status metro_op_gemm_fp8_plan(int32_t M, int32_t N, int32_t Kp, int32_t ep
                                     int64_t workspace_bytes, int32_t* kind, int32_t* w_rows, int32_t* x_rows,
                                     int32_t* k_slices) {
   clear_error();
-  if (!kind || !w_rows || !x_rows || !k_slices || M <= 0 || N <= 0 || N % 32 || Kp <= 0 || Kp % 128 || n_experts < 0 ||
-      workspace_bytes < 0 || (epilogue != metro::kEpi8Bf16 && epilogue != metro::kEpi8SwiGLU))
-    return report(METRO_E_INVAL, "gemm_fp8_plan: bad shape (N %% 32, Kp %% 128), epilogue or NULL output");
-  if (too_large(M, N, n_experts))
-    return report(METRO_E_INVAL, "gemm_fp8_plan: more than 2^26 rows, N 2^30, 2^36 results or %d experts", metro::kGemmFp8MaxExperts);
-  static const int32_t some = 0;
-  metro::GemmFp8Args a{};
-  a.offsets = n_experts ? &some : nullptr;  // (not read)
-  a.E = n_experts ? n_experts : 1;
-  a.M = M, a.N = N, a.Kp = a.ldx = Kp;
-  a.ws_floats = workspace_bytes / 4;
-  const metro::GemmFp8Plan p = metro::plan_gemm_fp8(a, epilogue);
+  metro::GemmFp8Plan p;
+  const metro_status st = plan_of("gemm_fp8_plan", M, N, Kp, epilogue, n_experts, workspace_bytes,
+                                  kind && w_rows && x_rows && k_slices, p);
+  if (st != METRO_OK) return st;
   const int waves = p.kind == metro::GemmFp8Kind::kTiled ? 2 : 1;
   *kind = static_cast<int32_t>(p.kind);
   *w_rows = 16 * p.nt * waves;
   *x_rows = 16 * p.mt * waves;
   *k_slices = p.ks;
   return METRO_OK;
+}
+
+metro_status metro_op_gemm_fp8_plan_bypass(int32_t M, int32_t N, int32_t Kp, int32_t epilogue, int32_t n_experts,
+                                           int64_t workspace_bytes, int32_t* w_bypass) {
+  clear_error();
+  metro::GemmFp8Plan p;
+  const metro_status st =
+      plan_of("gemm_fp8_plan_bypass", M, N, Kp, epilogue, n_experts, workspace_bytes, w_bypass != nullptr, p);
+  if (st == METRO_OK) *w_bypass = p.nt_hint;
+  return st;
 }
 
 metro_status metro_op_route(const float* logits, int32_t ldl, const float* bias, int32_t T, int32_t n_experts,

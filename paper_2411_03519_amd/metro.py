@@ -88,6 +88,7 @@ _SIGS = {
     "metro_op_gemm_fp8": (_i32, [_vp, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _i32, _vp, _i32, _vp,
                                  _i64, _vp]),
     "metro_op_gemm_fp8_plan": (_i32, [_i32, _i32, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _vp]),
+    "metro_op_gemm_fp8_plan_bypass": (_i32, [_i32, _i32, _i32, _i32, _i32, _i64, _vp]),
     "metro_op_route": (_i32, [_vp, _i32, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, ctypes.c_float, _vp, _vp, _vp, _vp,
                               _vp, _vp, _i64, _vp]),
     "metro_op_gemm_fp8_experts": (_i32, [_vp, _i32, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32, _vp,
@@ -414,6 +415,13 @@ def op_gemm_fp8_plan(M: int, N: int, Kp: int, epilogue: int, n_experts: int = 0,
     v = [ctypes.c_int32() for _ in range(4)]
     check(lib.metro_op_gemm_fp8_plan(M, N, Kp, epilogue, n_experts, workspace_bytes, *[ctypes.byref(x) for x in v]))
     return GEMM_FP8_KINDS[v[0].value], v[1].value, v[2].value, v[3].value
+
+
+def op_gemm_fp8_plan_bypass(M: int, N: int, Kp: int, epilogue: int, n_experts: int = 0, workspace_bytes: int = 0) -> bool:
+    """Whether the weights of that product would pass the caches by; host only."""
+    v = ctypes.c_int32()
+    check(lib.metro_op_gemm_fp8_plan_bypass(M, N, Kp, epilogue, n_experts, workspace_bytes, ctypes.byref(v)))
+    return bool(v.value)
 
 
 def op_route(logits, T: int, n_experts: int, top_k: int, experts, weights, offsets, src, slot, bias=None,
