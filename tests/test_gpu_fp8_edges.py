@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import fp8
-from tests.test_gpu_fp8_ops import check_rows8, dev, filled, host, metro, padded, workspace  # noqa: F401
+from tests.test_gpu_fp8_ops import check_rows8, dev, filled, host, metro, normal_rows, padded, workspace  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +81,46 @@ def test_swiglu_of_one_very_negative_row_leaves_the_others(metro):
         outs.append((np.delete(host(out), 7, 0), np.delete(host(scale), 7, 0)))
     np.testing.assert_array_equal(outs[0][0], outs[1][0])
     np.testing.assert_array_equal(outs[0][1], outs[1][1])
+
+
+# --- the norm whose sum nobody keeps ------------------------------------------------------
+
+
+@pytest.mark.parametrize("rows,d", [(1, 4096), (7, 300), (40, 8192)])
+def test_rmsnorm_adds_without_storing_the_sum(metro, rows, d):
+    rng = np.random.default_rng(d)
+    x = dev(rng.normal(size=(rows, d)).astype(np.float32))
+    delta = torch.from_numpy(rng.normal(size=(rows, d)).astype(np.float32)).cuda().to(torch.bfloat16)
+    g = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    before, D = x.clone(), -(-d // 128) * 128
+    outs = []
+    for keep in (torch.empty_like(x), None):
+        h, hs = filled((rows, D)), filled((rows, -(-D // 512) * 4))
+        metro.op_rmsnorm_fp8(x, g, 1e-5, h, hs, rows, d, delta=delta, x_out=keep)
+        outs.append((h, hs))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1]) and torch.equal(x, before)
+    want = fp8.rms_norm(host(x).astype(np.float64) + host(delta.float()), np.ones(d), 1e-5)
+    check_rows8(host(outs[1][0]), host(outs[1][1])[:, :D // 128], want)
+
+
+# --- the matrix cores' sums -------------------------------------------------------------
+
+
+@pytest.mark.parametrize("M,N,K,kind,ks", [(1, 32, 4736, "stream", 8), (33, 32, 2688, "tiled", 4), (69, 4224, 8960, "tiled", 8)])
+def test_sums_of_normal_data_before_their_rounding(metro, M, N, K, kind, ks):
+    """The k slices' fp32 sums, which stay in the workspace, against float64.  A product of two codes has 8 significant
+    bits, so one within 2^5 of the largest of its eight is kept whole and a smaller one is cut by less than 2^-13 of
+    the largest.  For normal data a sixth of the products is that small (|xy| < 0.07, of which the largest of eight
+    is 2.2 in the mean): sqrt(1/6) * 2.2 * 2^-13 / sqrt(3) = 6.3e-5 of the result's 2-norm, at most."""
+    epilogue = metro.EPI_FP8_SWIGLU if M == 69 else metro.EPI_FP8_BF16
+    ws = workspace(M, N)
+    assert metro.op_gemm_fp8_plan(M, N, K, epilogue, 0, 4 * ws.numel())[::3] == (kind, ks)
+    rng = np.random.default_rng([M, N, K])
+    x, w = normal_rows(rng, M, K), normal_rows(rng, N, K, 0.02)
+    G = -(-(N // 2) // 128)
+    out, scale = filled((M, G * 128 if epilogue else 2 * N)), filled((M, -(-G // 4) * 4))
+    metro.op_gemm_fp8(dev(x[0]), dev(padded(x[1])), dev(fp8.packed_codes(w[0])), dev(fp8.packed_bytes(w[1], 0xFF)), M, N, K,
+                      epilogue, out, out_scale=scale if epilogue else None, workspace=ws)
+    got = host(ws[:ks * M * N].reshape(ks, M, N)).astype(np.float64).sum(0)
+    want = fp8.values(*x) @ fp8.values(*w).T
+    assert np.linalg.norm(got - want) <= 6.4e-5 * np.linalg.norm(want)

@@ -94,3 +94,16 @@ def test_route_shut_out_experts_of_any_logit_have_no_weight(metro, T, value):
         got = check_route(metro, z, 4, [-np.inf, 0, -np.inf, 0], scoring=1, scale=2.0)
         assert (got[0] == [3, 1, 0, 2]).all() and (got[1][:, 2:] == 0).all()
         check_route(metro, z, 4, [-np.inf, 0, -np.inf, 0], scoring=1, renormalise=False)
+
+
+@pytest.mark.parametrize("T", [3, 70])
+def test_route_infinite_logits(metro, T):
+    """+inf in a softmax row makes its weights NaN, and under sigmoid a score of 1."""
+    z = np.random.default_rng(T).normal(size=(T, 16))
+    z[1, 4] = np.inf
+    for groups, top in ((1, 1), (4, 2)):
+        with np.errstate(all="ignore"):
+            got = check_route(metro, z, 4, n_groups=groups, top_groups=top)
+            assert np.isnan(got[1][1]).all() and np.isfinite(np.delete(got[1], 1, 0)).all()
+            got = check_route(metro, z, 4, scoring=1, n_groups=groups, top_groups=top, renormalise=False)
+            assert got[0][1, 0] == 4 and got[1][1, 0] == 1
