@@ -1,8 +1,10 @@
 /*
- * metro_ops.h -- single kernels of libmetro.so's forward pass, exported so
- * that each can be checked on its own against a CPU reference.  The model
- * entry points in metro.h are what a serving loop calls; these run one step
- * of it on caller-owned device buffers.
+ * metro_ops.h -- single operators on caller-owned device buffers: the kernels
+ * of libmetro.so's forward pass, exported so that each can be checked on its
+ * own against a CPU reference (the model entry points in metro.h are what a
+ * serving loop calls; these run one step of it), and the feed-forward block in
+ * 8 bits, which that forward pass (bf16 throughout) does not use: it is for
+ * callers that run layers of their own.
  *
  * All pointers are device pointers on the current HIP device; work is
  * enqueued on `stream` (a hipStream_t, NULL = default stream).  Return value
@@ -159,13 +161,15 @@ metro_status metro_op_attn_decode_noalloc(const uint16_t* q, const uint16_t* kv,
  * filled group are zero codes; bytes of a row's stride behind its last group
  * are left as they were, and no result hangs on what they hold.
  *
- * The feed-forward block of a Llama layer in them: metro_op_rmsnorm_fp8 (adds
- * the attention's output projection to the residual), metro_op_gemm_fp8 with
- * gate and up (SwiGLU), metro_op_gemm_fp8 with down (bf16 rows, which the next
- * layer's metro_op_rmsnorm_fp8 adds).  By experts: metro_op_rmsnorm_fp8 (with
- * h_bf16), metro_op_gemm with the router's weights, metro_op_route,
- * metro_op_gemm_fp8_experts with gate and up and src, the same with down, and
- * metro_op_combine_experts.
+ * The feed-forward block of a Llama layer in them: metro_op_rmsnorm_fp8,
+ * metro_op_gemm_fp8 with gate and up (SwiGLU), metro_op_gemm_fp8 with down (bf16
+ * rows, which the next layer's metro_op_rmsnorm_fp8 adds as its delta).  The
+ * attention's output projection in bf16 weights adds itself to the residual
+ * (metro_op_gemm, epilogue 1), and the norm behind it takes no delta.  By
+ * experts: metro_op_rmsnorm_fp8 (with h_bf16), metro_op_gemm with the router's
+ * weights, metro_op_route, metro_op_gemm_fp8_experts with gate and up and src,
+ * the same with down, and metro_op_combine_experts.  Rows of a QKV product come
+ * out plain: RoPE and the write of KV pages are steps of the model alone.
  *
  * All are asynchronous on `stream`, allocate nothing and may be captured into a
  * graph; a workspace belongs to one call at a time.  Calls of no rows (no tokens,

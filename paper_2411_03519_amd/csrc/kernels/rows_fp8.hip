@@ -118,7 +118,8 @@ hipError_t launch_rmsnorm_fp8(const NormFp8Args& a, hipStream_t s) {
 
 // ---------------------------------------------------------------------------
 // Weights, once at loading: a wave quantises one group (row n, 128 columns), two
-// values a lane.  Columns K .. Kp - 1 are zero codes.
+// values a lane.  Columns K .. Kp - 1 are zero codes.  Bound by its accesses of two
+// bytes a lane: 28672 x 4096 222 us, 1.6 TB/s of bytes that 61 us would move.
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void pack_weight_fp8_kernel(const uint16_t* __restrict__ src, int64_t ld, int N, int K,
                                                               int Kp, uint8_t* __restrict__ dst,
