@@ -311,6 +311,133 @@ metro_status metro_op_combine_experts(const uint16_t* y, int32_t ldy, int32_t y_
                                       const int32_t* slot, int32_t T, int32_t top_k, int32_t d, const float* resid,
                                       float* out, int32_t ldo, void* stream);
 
+/* --- a speculative decoding step ---------------------------------------------
+ *
+ * What a layer does with rows of a QKV product, for callers that run layers of
+ * their own (metro_op_gemm, metro_op_gemm_fp8) over pages of the layout above:
+ * metro_op_rope_append puts the drafted tokens' keys and values into the cache and
+ * leaves their queries, metro_op_attn_tree attends over both, and behind the
+ * head's product metro_op_sample chooses a token at every drafted one.  The
+ * drafts whose tokens agree are accepted; metro_op_kv_move brings their keys and
+ * values, in all layers, to the slots behind the context.  One token a sequence
+ * without drafts is the case of one query an item, a prompt's chunk that of a
+ * chain of them.
+ *
+ * All are asynchronous on `stream`, allocate nothing and may be captured into a
+ * graph; a workspace belongs to one call at a time.  Calls of no rows (items,
+ * moves) do nothing; buffers that would hold no element may be NULL.  Index arrays
+ * are read on the device and held to their ranges there: an index outside touches
+ * nothing outside the buffers. */
+
+/* Rows of a QKV product into the cache.  Of row t, head by head (nq query heads,
+ * nkv key heads, nkv value heads of hd columns each, in plain order):
+ *   y <- y / sqrt(mean(y^2) + eps) * gain     query heads with q_gain, key heads
+ *                                             with k_gain (NULL: no norm)
+ *   (y_i, y_{i+hd/2}) <- (y_i c - y_{i+hd/2} s, y_i s + y_{i+hd/2} c),  i < hd/2,
+ *                  (c, s) = rope[pos[t], i]   query and key heads
+ * in fp32, rounded to bf16 once: queries to q[t], keys and values to the cache's
+ * slot[t] (page * 16 + offset).  A row whose slot lies outside 0 .. 16 n_pages - 1
+ * (a padded batch's) leaves the cache as it is, its queries are written all the
+ * same.  A position outside 0 .. n_pos - 1 makes the row's queries and keys NaN.
+ * Slots of different rows differ; of rows with the same slot the cache keeps
+ * values of one or the other.
+ *   qkv_f32, qkv_bf16  device [T, ld], one of them, the other NULL; 16-byte aligned,
+ *             ld % 8 == 0, ld >= (nq + 2 nkv) hd
+ *   q_gain, k_gain  device bf16 [hd] or NULL, 16-byte aligned
+ *   rope      device fp32 [n_pos, hd / 2, 2], 16-byte aligned
+ *   pos, slot device int32 [T]
+ *   q         device bf16 [T, nq, hd], 16-byte aligned
+ *   kv        device bf16, n_pages pages in the layout above, 16-byte aligned
+ * hd 64 or 128, nq <= 1024, nkv <= 256, T * (nq + 2 nkv) <= 2^25, n_pages < 2^27.
+ * Errors: E_INVAL. */
+metro_status metro_op_rope_append(const float* qkv_f32, const uint16_t* qkv_bf16, int32_t ld, int32_t T, int32_t nq,
+                                  int32_t nkv, int32_t hd, const uint16_t* q_gain, const uint16_t* k_gain, float eps,
+                                  const float* rope, int32_t n_pos, const int32_t* pos, const int32_t* slot, uint16_t* q,
+                                  uint16_t* kv, int32_t n_pages, void* stream);
+
+/* Keys and values from slot to slot of the cache, in n_layers layers whose pages
+ * lie layer_stride elements apart: for each group g of moves and j = offsets[g] ..
+ * offsets[g+1] - 1 in order, dst[j] <- src[j], as if all sources of a group were
+ * read before its first destination is written (groups of more than 32 moves: of
+ * 32 at a time, in order, which is the same where a group's moves rise and none
+ * goes up, dst[j] <= src[j]).  A later move of a group to the same slot wins.  A
+ * slot that one group writes is neither read nor written by another.  Moves from
+ * or to a slot outside 0 .. 16 n_pages - 1 are left out.
+ *   kv        device bf16, 16-byte aligned; layer_stride % 8 == 0, at least n_pages
+ *             pages (not looked at for one layer)
+ *   src, dst  device int32 [n_moves];  offsets  device int32 [n_groups + 1],
+ *             ascending, within 0 .. n_moves
+ * hd 64 or 128, nkv <= 256, n_layers and n_groups <= 65535.  Errors: E_INVAL. */
+metro_status metro_op_kv_move(uint16_t* kv, int64_t layer_stride, int32_t n_layers, int32_t n_pages, int32_t nkv, int32_t hd,
+                              const int32_t* src, const int32_t* dst, const int32_t* offsets, int32_t n_groups,
+                              int32_t n_moves, void* stream);
+
+/* Attention of drafted tokens over the cache.  Item i has the query rows cu_q[i] ..
+ * cu_q[i+1] - 1, n of them, and its pages hold keys 0 .. ctx[i] + n - 1, the last n
+ * those of the queries in their order.  Query r of the item sees keys 0 .. ctx[i] -
+ * 1 and key ctx[i] + j where bit j % 32 of mask[row, j / 32] is set (mask NULL: for
+ * j <= r, a chain); over the keys t that it sees, as metro_op_attn_decode,
+ *   out[row, head, :] = bf16( sum_t softmax_t(q . K[t] / sqrt(hd)) V[t] ),
+ * zeros where it sees none, or none whose score is above -inf.  What the keys that
+ * a query does not see hold (NaN, Inf) does not reach it.  Rows in no item are left
+ * as they were.
+ *   q         device bf16 [rows, nq, hd], 16-byte aligned
+ *   kv        device bf16, n_pages pages in the layout above, 16-byte aligned
+ *   cu_q      device int32 [n_items + 1], ascending, within 0 .. rows
+ *   ctx       device int32 [n_items], >= 0
+ *   max_q     most queries of an item, 1 .. 4096; later ones are left as they were
+ *   max_keys  most keys of an item (ctx + its queries); keys from there on are not
+ *             seen.  The larger it is beside the items' own, the fewer workgroups
+ *             share the keys there are
+ *   mask      device uint32 [rows, ldm] or NULL, 32 * ldm >= max_q
+ *   block_tables  device int32 [n_items, ldb] page ids, 16 * ldb >= max_keys
+ *   out       device bf16 [rows, nq * hd], 16-byte aligned, not q
+ *   workspace NULL, or device fp32 of workspace_bytes, 16-byte aligned: what
+ *             metro_op_attn_tree_workspace says lets the keys of an item be split
+ *             over workgroups as the call's size asks for, less gives fewer splits,
+ *             NULL none.  Which splits run follows from the sizes and
+ *             workspace_bytes, and their states are merged in order, so results of
+ *             equal calls are equal bit for bit
+ * hd 64 or 128, nq / nkv 1, 2, 4 or 8, nkv <= 256, n_items * max_q <= 2^22 and
+ * n_items * nkv * ceil(max_q * nq / nkv / 16) <= 2^22.  Errors: E_INVAL. */
+metro_status metro_op_attn_tree(const uint16_t* q, const uint16_t* kv, int32_t n_pages, int32_t nq, int32_t nkv, int32_t hd,
+                                int32_t n_items, const int32_t* cu_q, int32_t rows, const int32_t* ctx, int32_t max_q,
+                                int32_t max_keys, const uint32_t* mask, int32_t ldm, const int32_t* block_tables,
+                                int32_t ldb, uint16_t* out, float* workspace, int64_t workspace_bytes, void* stream);
+
+/* *bytes: the workspace that metro_op_attn_tree makes use of; host only. */
+metro_status metro_op_attn_tree_workspace(int32_t nq, int32_t nkv, int32_t hd, int32_t n_items, int32_t rows, int32_t max_q,
+                                          int32_t max_keys, int64_t* bytes);
+
+/* Sampled choice of a token of each row.  With x = logits[r, 0 .. vocab - 1], the
+ * tokens in the order of falling x, ties by rising index, and in fp64
+ *   w = exp((x - max x) / temperature[r])        (1 where x is the largest)
+ *   min-p  keeps the tokens with w >= min_p[r]   (<= 0: all; >= 1: those of w = 1)
+ *   top-k  keeps the first top_k[r] of them      (<= 0: all)
+ *   top-p  keeps the shortest beginning of them whose sum of w is at least top_p[r]
+ *          of theirs, one token at the least     (>= 1: all)
+ *   out[r] = the first token of the order whose sum of w up to and with it is above
+ *          u[r] times the sum of the kept ones
+ *   prob[r] = its w / that sum, unless prob is NULL
+ * so u = 0 gives the most likely token, and u uniform on [0, 1) samples.  u below 0
+ * or NaN counts as 0, from 1 on it gives the last kept token.  Weights below 2^-46
+ * count as none (of 2^18 they change the sums by less than 2^-28).  temperature 0,
+ * below 0 or NaN is the greedy choice (metro_op_argmax, prob 1).  A NaN setting
+ * otherwise counts as not set; a NULL array sets none (temperature 1).  NaN logits
+ * are skipped; out is -1 and prob 0 where none is above -inf.
+ *   logits  device fp32 [rows, ldl], ldl >= vocab
+ *   temperature, top_p, min_p, u  device fp32 [rows];  top_k, out  device int32 [rows]
+ *   prob    device fp32 [rows] or NULL
+ *   workspace  device, 16-byte aligned, of at least what metro_op_sample_workspace says
+ * Results do not depend on the order in which anything is added.  vocab <= 2^18, rows
+ * <= 65535.  Errors: E_INVAL. */
+metro_status metro_op_sample(const float* logits, int32_t ldl, int32_t rows, int32_t vocab, const float* temperature,
+                             const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* out,
+                             float* prob, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* *bytes: the workspace that metro_op_sample needs; host only. */
+metro_status metro_op_sample_workspace(int32_t rows, int32_t vocab, int64_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,6 +33,10 @@ SOURCES = [
     "csrc/kernels/rows_fp8.hip",
     "csrc/kernels/route.hip",
     "csrc/kernels/gemm_fp8.hip",
+    "csrc/ops_draft.hip",
+    "csrc/kernels/append.hip",
+    "csrc/kernels/attn_tree.hip",
+    "csrc/kernels/sample.hip",
 ]
 
 ARCH = "gfx950"

@@ -94,6 +94,14 @@ _SIGS = {
     "metro_op_gemm_fp8_experts": (_i32, [_vp, _i32, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32, _vp,
                                          _vp, _i32, _vp, _i32, _vp, _i64, _vp]),
     "metro_op_combine_experts": (_i32, [_vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _i32, _vp]),
+    "metro_op_rope_append": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, ctypes.c_float, _vp, _i32, _vp, _vp,
+                                    _vp, _vp, _i32, _vp]),
+    "metro_op_kv_move": (_i32, [_vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _i32, _i32, _vp]),
+    "metro_op_attn_tree": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _i32, _vp, _i32, _i32, _vp, _i32, _vp, _i32,
+                                  _vp, _vp, _i64, _vp]),
+    "metro_op_attn_tree_workspace": (_i32, [_i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp]),
+    "metro_op_sample": (_i32, [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "metro_op_sample_workspace": (_i32, [_i32, _i32, _vp]),
     "metro_sched_create": (_i32, [_vp, _vp, ctypes.POINTER(_vp)]),
     "metro_sched_destroy": (None, [_vp]),
     "metro_sched_next": (_i32, [_vp, ctypes.POINTER(_i32), ctypes.POINTER(_i32), _vp, _i32, ctypes.POINTER(_i32)]),
@@ -449,6 +457,57 @@ def op_combine_experts(y, y_rows: int, weights, slot, T: int, top_k: int, d: int
     """out = resid + the weighted sum of each token's slots of y."""
     check(lib.metro_op_combine_experts(_ptr(y), d if ldy is None else ldy, y_rows, _ptr(weights), _ptr(slot), T, top_k, d,
                                        _ptr(resid), _ptr(out), d if ldo is None else ldo, _stream(stream)))
+
+
+# -- a speculative decoding step (see metro_ops.h); index arrays are int32 device tensors
+
+def op_rope_append(qkv, T: int, nq: int, nkv: int, hd: int, rope, n_pos: int, pos, slot, q, kv, n_pages: int, q_gain=None,
+                   k_gain=None, eps: float = 1e-5, ld: int | None = None, stream=None):
+    """Rows of a QKV product (float32 or bfloat16) -> rotated queries q and keys and
+    values in the cache's slots, normalised by head where a gain is given."""
+    half = qkv is not None and qkv.element_size() == 2
+    check(lib.metro_op_rope_append(None if half else _ptr(qkv), _ptr(qkv) if half else None,
+                                   (nq + 2 * nkv) * hd if ld is None else ld, T, nq, nkv, hd, _ptr(q_gain), _ptr(k_gain),
+                                   eps, _ptr(rope), n_pos, _ptr(pos), _ptr(slot), _ptr(q), _ptr(kv), n_pages,
+                                   _stream(stream)))
+
+
+def op_kv_move(kv, n_layers: int, n_pages: int, nkv: int, hd: int, src, dst, offsets, n_groups: int, n_moves: int,
+               layer_stride: int | None = None, stream=None):
+    """Keys and values of slots src to slots dst of the cache, in every layer."""
+    check(lib.metro_op_kv_move(_ptr(kv), n_pages * 32 * nkv * hd if layer_stride is None else layer_stride, n_layers, n_pages,
+                               nkv, hd, _ptr(src), _ptr(dst), _ptr(offsets), n_groups, n_moves, _stream(stream)))
+
+
+def op_attn_tree_workspace(nq: int, nkv: int, hd: int, n_items: int, rows: int, max_q: int, max_keys: int) -> int:
+    """Bytes of workspace that op_attn_tree makes use of; host only."""
+    n = ctypes.c_int64()
+    check(lib.metro_op_attn_tree_workspace(nq, nkv, hd, n_items, rows, max_q, max_keys, ctypes.byref(n)))
+    return n.value
+
+
+def op_attn_tree(q, kv, n_pages: int, nq: int, nkv: int, hd: int, n_items: int, cu_q, rows: int, ctx, max_q: int,
+                 max_keys: int, block_tables, ldb: int, out, mask=None, ldm: int = 0, workspace=None, stream=None):
+    """Attention of each item's queries over its cached keys and the drafted ones
+    that mask names (None: a chain)."""
+    check(lib.metro_op_attn_tree(_ptr(q), _ptr(kv), n_pages, nq, nkv, hd, n_items, _ptr(cu_q), rows, _ptr(ctx), max_q,
+                                 max_keys, _ptr(mask), ldm, _ptr(block_tables), ldb, _ptr(out), _ptr(workspace),
+                                 _bytes(workspace), _stream(stream)))
+
+
+def op_sample_workspace(rows: int, vocab: int) -> int:
+    """Bytes of workspace that op_sample needs; host only."""
+    n = ctypes.c_int64()
+    check(lib.metro_op_sample_workspace(rows, vocab, ctypes.byref(n)))
+    return n.value
+
+
+def op_sample(logits, rows: int, vocab: int, u, out, temperature=None, top_k=None, top_p=None, min_p=None, prob=None,
+              ldl: int | None = None, workspace=None, stream=None):
+    """A token of each row of logits from the uniform numbers u, and its probability."""
+    check(lib.metro_op_sample(_ptr(logits), vocab if ldl is None else ldl, rows, vocab, _ptr(temperature), _ptr(top_k),
+                              _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(out), _ptr(prob), _ptr(workspace), _bytes(workspace),
+                              _stream(stream)))
 
 
 # ----------------------------------------------------------------------------
