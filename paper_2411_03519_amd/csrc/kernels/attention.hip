@@ -51,19 +51,6 @@ __device__ __forceinline__ f32x4 mfma_k16(uint2 a, uint2 b, f32x4 c) {
                                                    0, 0, 0);
 }
 
-// The upper half of a trades places with the lower half of b.  An MFMA that
-// reads the result has to be at least two instructions away (wait states that
-// the compiler does not add behind inline assembly): NOPS of them are part of
-// the block, the caller keeps the others between.
-template <int NOPS>
-__device__ __forceinline__ void swap_halves(uint4& a, uint4& b) {
-  if constexpr (NOPS == 2)
-    asm volatile("v_swap_b32 %0, %2\n\tv_swap_b32 %1, %3\n\ts_nop 1"
-                 : "+v"(a.z), "+v"(a.w), "+v"(b.x), "+v"(b.y));
-  else
-    asm volatile("v_swap_b32 %0, %2\n\tv_swap_b32 %1, %3" : "+v"(a.z), "+v"(a.w), "+v"(b.x), "+v"(b.y));
-}
-
 // 2^x by the hardware instruction (v_exp_f32, about 1 ulp).  exp2f adds a
 // range fix-up (compare, two selects, ldexp) that only matters for results
 // below 2^-126; here x = s - m <= 0 is a softmax exponent, and such a weight

@@ -100,6 +100,21 @@ __host__ __device__ __forceinline__ int64_t packed_offset(int64_t n, int64_t k, 
   return ((((n >> 4) * (Kp >> 5) + (k >> 5)) * 64 + (n & 15) + 16 * ((k >> 3) & 3)) << 3) + (k & 7);
 }
 
+// --- V^T operands of a page pair ----------------------------------------------
+
+// The upper half of a trades places with the lower half of b.  An MFMA that
+// reads the result has to be at least two instructions away (wait states that
+// the compiler does not add behind inline assembly): NOPS of them are part of
+// the block, the caller keeps the others between.
+template <int NOPS>
+__device__ __forceinline__ void swap_halves(uint4& a, uint4& b) {
+  if constexpr (NOPS == 2)
+    asm volatile("v_swap_b32 %0, %2\n\tv_swap_b32 %1, %3\n\ts_nop 1"
+                 : "+v"(a.z), "+v"(a.w), "+v"(b.x), "+v"(b.y));
+  else
+    asm volatile("v_swap_b32 %0, %2\n\tv_swap_b32 %1, %3" : "+v"(a.z), "+v"(a.w), "+v"(b.x), "+v"(b.y));
+}
+
 // --- direct loads into LDS ---------------------------------------------------
 // global_load_lds_dwordx4 writes each lane's 16 bytes at LDS base + 16 * lane
 // (base in M0, wave-uniform) and counts in vmcnt like any vector load.  The

@@ -52,11 +52,11 @@ struct TreeArgs {
   int items, rows, nq, nkv, hd, n_pages, max_q, max_keys, ldm, ldb;
 };
 constexpr int kTreeMaxQ = 4096;  // queries of an item
-// How the cache's keys are cut: `splits` parts of `pairs` page pairs each.
+// How a call is cut: `tiles` tiles of `wide` columns (query, head of a group) for each item and kv head, and the keys
+// into `splits` parts of `pairs` page pairs.
 struct TreePlan {
-  int ct;      // 16-column tiles of a workgroup
-  int splits;
-  int pairs;
+  int wide, tiles;
+  int splits, pairs;
 };
 TreePlan plan_attn_tree(int nq, int nkv, int hd, int items, int rows, int max_q, int max_keys, int64_t part_floats);
 hipError_t launch_attn_tree(const TreeArgs& a, hipStream_t s);
