@@ -420,8 +420,9 @@ metro_status metro_op_attn_tree_workspace(int32_t nq, int32_t nkv, int32_t hd, i
  *          u[r] times the sum of the kept ones
  *   prob[r] = its w / that sum, unless prob is NULL
  * so u = 0 gives the most likely token, and u uniform on [0, 1) samples.  u below 0
- * or NaN counts as 0, from 1 on it gives the last kept token.  Weights below 2^-46
- * count as none (of 2^18 they change the sums by less than 2^-28).  temperature 0,
+ * or NaN counts as 0, from 1 on it gives the last kept token.  Weights are
+ * held to 2^-35 of themselves, those below 2^-46 may count as none (of 2^18 they
+ * change the sums by less than 2^-28).  temperature 0,
  * below 0 or NaN is the greedy choice (metro_op_argmax, prob 1).  A NaN setting
  * otherwise counts as not set; a NULL array sets none (temperature 1).  NaN logits
  * are skipped; out is -1 and prob 0 where none is above -inf.

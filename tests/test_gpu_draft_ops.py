@@ -12,9 +12,9 @@ Tolerances count roundings of half a step: 2^-8 of the value for bf16, 2^-24 for
   weights, of which 2^-16 is the rest behind the pair hi + lo that enters the matrix
   cores and the others are the fp32 scores' (|z| <= 32 in these cases: 2^-24 * 32
   times the few roundings of a sum of 128, within 2^-16) and the sums'.
-* sample: tokens are equal; prob rounds once to fp32 (2^-24 of it) from weights held
-  as multiples of 2^-45, half a step 2^-46, of sums that are at least 1: 2^-24 prob +
-  2^-28 with 2^18 of them.
+* sample: tokens are equal; prob rounds once to fp32 (2^-24 of it) from weights and
+  sums of relative error 2^-35 (half a step of 2^-34 next to 1), of which those below
+  e^-32 < 2^-46 of the largest may be missing: 2^-24 prob + 2^-28 with 2^18 of them.
 * kv_move and whatever is to be left alone: equal bit for bit.
 """
 
