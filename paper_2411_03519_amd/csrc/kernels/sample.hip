@@ -27,12 +27,16 @@
 #include "kernels.h"
 #include "kernels_draft.h"
 
+// Bins and weights of a logit are formed in several places and have to be the same in all of them: products and sums
+// are joined to one rounding only where the code says so.
+#pragma clang fp contract(off)
+
 namespace metro {
 
 constexpr int kSampleThreads = 1024;
 constexpr int kSampleBins = 1024;
 constexpr int kSampleChunk = 16384;  // logits of a workgroup, 16 a thread
-constexpr int kSampleList = 256;     // tokens that are listed, and that are ranked by comparing all pairs
+constexpr int kSampleList = 256;     // tokens of a chunk that are listed
 constexpr int kSampleChunks = kSampleMaxVocab / kSampleChunk;
 constexpr int kMassBits = 49;  // of a bin's word, the count above them: 16384 * 2^34 < 2^49
 constexpr uint64_t kMassMask = (1ull << kMassBits) - 1;
@@ -99,7 +103,7 @@ __device__ __forceinline__ void lds_add(uint64_t* p, uint64_t v) {
   atomicAdd(reinterpret_cast<unsigned long long*>(p), static_cast<unsigned long long>(v));
 }
 
-__global__ __launch_bounds__(kSampleThreads) void sample_chunk_kernel(SampleArgs a, int chunks) {
+__global__ __launch_bounds__(kSampleThreads, 8) void sample_chunk_kernel(SampleArgs a, int chunks) {
   constexpr int V = kSampleChunk / kSampleThreads;
   __shared__ uint64_t bin[kSampleBins];
   __shared__ SampleBest best[kSampleThreads / 64];
@@ -138,12 +142,12 @@ __global__ __launch_bounds__(kSampleThreads) void sample_chunk_kernel(SampleArgs
   if (tid == 0) out->max = b.v, out->index = b.i;
   if (!(t > 0.f) || !(b.v > -INFINITY)) return;  // (greedy, or nothing to choose: the rest is not read)
   const SampleGrid grid = sample_grid(b.v, t);
-  int at[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     uint64_t mass;
-    at[j] = sample_bin(grid, v[j], &mass);
-    if (at[j] >= 0) lds_add(&bin[at[j]], mass + (1ull << kMassBits));
+    const int at = sample_bin(grid, v[j], &mass);
+    if (at >= 0) lds_add(&bin[at], mass + (1ull << kMassBits));
+    if (j % 2) __builtin_amdgcn_sched_barrier(0);  // (two at a time: all at once take more than 64 registers)
   }
   __syncthreads();
   const uint64_t mine = bin[tid];
@@ -158,253 +162,110 @@ __global__ __launch_bounds__(kSampleThreads) void sample_chunk_kernel(SampleArgs
   __syncthreads();
   for (int w = 0; w < wave; ++w) n += sums[w];
   const int covered = __syncthreads_count(n <= kSampleList);
+  const double from = grid.top - covered + 1.0;  // (least t of the bins that are covered)
+#pragma unroll
+  for (int j = 0; j < V; ++j) asm volatile("" : "+v"(v[j]));  // (t is formed again, not held from above: 32 registers)
 #pragma unroll
   for (int j = 0; j < V; ++j)
-    if (at[j] >= 0 && at[j] < covered)
+    if (covered > 0 && (static_cast<double>(v[j]) * grid.per >= from || v[j] == b.v))
       out->list[atomicAdd(&n_list, 1)] = make_float2(v[j], __int_as_float(first + j / 4 * 4 * kSampleThreads + j % 4));
   __syncthreads();
   if (tid == 0) out->covered = covered, out->listed = n_list;
 }
 
+constexpr int kSampleGather = 4096;  // tokens that the second launch holds in LDS
+constexpr int kSampleRank = 96;      // tokens that are ranked by comparing all pairs
+
+constexpr int kSampleSearches = 8;   // for bins, each with room of its own
+
 struct SampleShared {
-  double before[kSampleBins], with[kSampleBins];  // weight of the bins above, and with this one
+  double before[kSampleBins], with[kSampleBins];    // weight of the bins above, and with this one
   uint32_t count[kSampleBins], above[kSampleBins];  // tokens of a bin, and of the bins above
-  double scan_w[16];
-  uint32_t scan_c[16];
   uint64_t sub_mass[kSampleBins];
   uint32_t sub_count[kSampleBins];
+  uint32_t key[kSampleGather];  // the gathered tokens
+  int index[kSampleGather];
+  uint16_t bin[kSampleGather];
+  uint8_t wanted[kSampleBins];  // bins that are gathered
+  uint32_t rank_key[kSampleRank];
+  int rank_index[kSampleRank];
+  uint64_t rank_mass[kSampleRank];
+  double scan_w[16];
   uint64_t scan_m[16];
-  uint32_t key[kSampleList];
-  int index[kSampleList];
-  uint64_t weight[kSampleList];
-  uint32_t n_list, key_lo, key_hi;
-  int bin, sub;
-  // what a search leaves: the sums up to the token and with it, the token's own weight and index
-  double upto;
+  uint32_t scan_c[16];
+  int scan_last[16];
+  uint32_t n, some_n;
   uint64_t some;
-  uint32_t tokens, some_n;
-  double own;
+  int first, sub;
+  int found_bin[kSampleSearches][kSampleThreads / 64];
+  // what a search leaves: the weights up to its token and with it, the token's own weight and index
+  double upto, own;
   int found;
-  int shift[kSampleChunks];  // bins between the row's largest and a chunk's, or so many that it has none
+  int shift[kSampleChunks];    // bins between the row's largest and a chunk's; all of them where it counts for nothing
   int covered[kSampleChunks];  // bins of a chunk whose tokens are listed
 };
 
 enum SampleWant { kByCount, kReach, kPass };  // the first token whose count, or weight, up to it reaches, or passes, the wanted
 
-struct SampleRow {
-  const float* x;
-  const SampleChunk* chunk;
-  int vocab, chunks, last_bin;
-  SampleGrid grid;
-
-  // the listed tokens of all chunks, four a thread (absent ones NaN)
-  static constexpr int L = kSampleChunks * kSampleList / kSampleThreads;
-  float listed[L];
-  int listed_at[L];
-
-  // f(logit, index) of the tokens that may be in a bin: the listed ones, where they hold all of it, else the row's.
-  template <typename F>
-  __device__ __forceinline__ void each(bool lists, F f) const {
-    if (lists) {
-#pragma unroll
-      for (int k = 0; k < L; ++k) f(listed[k], listed_at[k]);
-      return;
-    }
-    const int head = min(static_cast<int>(((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / 4), vocab);
-    const int n4 = (vocab - head) / 4, tail = head + 4 * n4;
-    if (static_cast<int>(threadIdx.x) < head) f(x[threadIdx.x], threadIdx.x);
-    if (static_cast<int>(threadIdx.x) < vocab - tail) f(x[tail + threadIdx.x], tail + threadIdx.x);
-    const float4* x4 = reinterpret_cast<const float4*>(x + head);
-    constexpr int U = 4;
-    for (int j0 = threadIdx.x; j0 < n4; j0 += U * kSampleThreads) {
-      float4 w[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) w[u] = x4[min(j0 + u * kSampleThreads, n4 - 1)];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int j = j0 + u * kSampleThreads, i = head + 4 * j;
-        if (j >= n4) continue;
-        f(w[u].x, i);
-        f(w[u].y, i + 1);
-        f(w[u].z, i + 2);
-        f(w[u].w, i + 3);
-      }
-    }
-  }
-  // whether every chunk lists its tokens of bin b
-  __device__ __forceinline__ bool at_hand(const SampleShared& sh, int b) const {
-    bool all = true;
-    for (int c = 0; c < chunks; ++c) all &= b < sh.shift[c] + sh.covered[c];
-    return all;
-  }
-};
-
 __device__ __forceinline__ double bin_scale(int b) { return exp(-b / 32.0) / kMassOne; }
 
-// The first token of the order whose count or weight up to it is as wanted; the last one where none is (a sum's rounding).
-__device__ void locate(SampleShared& sh, const SampleRow& r, SampleWant how, uint32_t count, double want, bool index) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (tid == 0) sh.bin = r.last_bin;
-  __syncthreads();
-  {
-    const double upto = sh.with[tid];
-    const bool ok = how == kByCount ? sh.above[tid] + sh.count[tid] >= count : how == kReach ? upto >= want : upto > want;
-    if (sh.count[tid] > 0 && ok) atomicMin(&sh.bin, tid);
-  }
-  __syncthreads();
-  const int bin = sh.bin;
-  const double before = sh.before[bin], scale = bin_scale(bin);
-  const uint32_t above = sh.above[bin];
-  const bool lists = r.at_hand(sh, bin);
-  auto there = [&](uint32_t c, uint64_t m) {
-    const double upto = before + static_cast<double>(m) * scale;
-    return how == kByCount ? above + c >= count : how == kReach ? upto >= want : upto > want;
+// The weight up to a token of a bin.  One rounding wherever it is formed, so that equal sums compare equal.
+__device__ __forceinline__ double weight_up_to(double before, uint64_t mass, double scale) {
+  return fma(static_cast<double>(mass), scale, before);
+}
+
+struct SampleRange {
+  float lo, hi;
+  __device__ __forceinline__ bool has(float v) const { return v >= lo && v <= hi; }
+};
+constexpr SampleRange kNoRange{INFINITY, -INFINITY};
+
+// f(logit, index) of a row's logits within either range.  The few that are, of 32 at a time, are marked first and then taken
+// one by one from memory again: tested where they are, nearly every wave would go through f for some lane.
+template <typename F>
+__device__ __forceinline__ void each_of_row(const float* x, int vocab, SampleRange a, SampleRange b, F f) {
+  const int tid = threadIdx.x;
+  const int head = min(static_cast<int>(((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / 4), vocab);
+  const int n4 = (vocab - head) / 4, tail = head + 4 * n4;
+  auto test = [&](int i) {
+    const float v = x[i];
+    if (a.has(v) || b.has(v)) f(v, i);
   };
-  uint64_t base_m = 0;  // of the bin's tokens above those of [lo, hi]
-  uint32_t base_c = 0, n = sh.count[bin], lo = 0, hi = 0xffffffffu;
-  auto mine = [&](float x, uint64_t* m) {
-    const uint32_t k = order_key(x);
-    return k >= lo && k <= hi && sample_bin(r.grid, x, m) == bin;
-  };
-  if (n > kSampleList) {
-    if (tid == 0) sh.key_lo = 0xffffffffu, sh.key_hi = 0;
-    __syncthreads();
-    uint32_t l = 0xffffffffu, u = 0;
-    r.each(lists, [&](float x, int) {
-      uint64_t m;
-      if (mine(x, &m)) l = min(l, order_key(x)), u = max(u, order_key(x));
-    });
-    atomicMin(&sh.key_lo, l);
-    atomicMax(&sh.key_hi, u);
-    __syncthreads();
-    lo = sh.key_lo, hi = sh.key_hi;
-  }
-  while (n > kSampleList && lo < hi) {
-    const int shift = max(0, 32 - __clz(hi - lo) - 10);  // (hi - lo) >> shift < 1024
-    __syncthreads();
-    sh.sub_mass[tid] = 0, sh.sub_count[tid] = 0;
-    __syncthreads();
-    r.each(lists, [&](float x, int) {
-      uint64_t m;
-      if (!mine(x, &m)) return;
-      const uint32_t b = (hi - order_key(x)) >> shift;
-      lds_add(&sh.sub_mass[b], m);
-      atomicAdd(&sh.sub_count[b], 1u);
-    });
-    if (tid == 0) sh.sub = -1;
-    __syncthreads();
-    const uint64_t m = sh.sub_mass[tid];
-    const uint32_t c = sh.sub_count[tid];
-    uint64_t im = m;
-    uint32_t ic = c;
+  if (tid < head) test(tid);
+  if (tid < vocab - tail) test(tail + tid);
+  const float4* x4 = reinterpret_cast<const float4*>(x + head);
+  constexpr int U = 8;
+  for (int j0 = tid; j0 < n4; j0 += U * kSampleThreads) {
+    float4 w[U];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint64_t pm = __shfl_up(static_cast<unsigned long long>(im), o, kWave);
-      const uint32_t pc = __shfl_up(ic, o, kWave);
-      if (lane >= o) im += pm, ic += pc;
-    }
-    if (lane == 63) sh.scan_m[wave] = im, sh.scan_c[wave] = ic;
-    __syncthreads();
-    im += base_m, ic += base_c;
-    for (int w = 0; w < wave; ++w) im += sh.scan_m[w], ic += sh.scan_c[w];
-    // the first that is as wanted, or the last that holds any
-    const bool first = c > 0 && there(ic, im) && (ic - c == base_c || !there(ic - c, im - m));
-    if (c > 0) atomicMax(&sh.sub, tid);
-    __syncthreads();
-    if (first) sh.sub = -2 - tid;
-    __syncthreads();
-    const int sub = sh.sub <= -2 ? -2 - sh.sub : sh.sub;
-    __syncthreads();
-    if (tid == sub) sh.some = im - m, sh.some_n = ic - c;
-    __syncthreads();
-    base_m = sh.some, base_c = sh.some_n, n = sh.sub_count[sub];
-    const uint64_t top = hi, from = (static_cast<uint64_t>(sub) + 1) << shift;
-    lo = top + 1 > from ? max(lo, static_cast<uint32_t>(top + 1 - from)) : lo;
-    hi = static_cast<uint32_t>(top - (static_cast<uint64_t>(sub) << shift));
-  }
-  __syncthreads();
-  if (n > kSampleList) {  // all the same
-    uint64_t w;
-    sample_bin(r.grid, key_value(hi), &w);
-    uint32_t nth = 1;  // the least that is as wanted, by halves: `there` only ever turns true
-    for (uint32_t l = 1, h = n; l < h;) {
-      const uint32_t mid = l + (h - l) / 2;
-      if (there(base_c + mid, base_m + mid * w)) h = mid;
-      else l = mid + 1;
-      nth = l;
-    }
-    if (tid == 0) {
-      sh.upto = before + static_cast<double>(base_m + nth * w) * scale;
-      sh.tokens = above + base_c + nth;
-      sh.own = static_cast<double>(w) * scale;
-    }
-    if (index) {
-      const int chunk = (r.vocab + kSampleThreads - 1) / kSampleThreads, i0 = tid * chunk, i1 = min(i0 + chunk, r.vocab);
-      const float same = key_value(hi);
-      uint32_t c = 0;
-      for (int i = i0; i < i1; ++i) c += r.x[i] == same ? 1 : 0;
-      uint32_t ic = c;
+    for (int u = 0; u < U; ++u) w[u] = x4[min(j0 + u * kSampleThreads, n4 - 1)];
+    uint32_t in = 0;
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t pc = __shfl_up(ic, o, kWave);
-        if (lane >= o) ic += pc;
-      }
-      if (lane == 63) sh.scan_c[wave] = ic;
-      __syncthreads();
-      for (int k = 0; k < wave; ++k) ic += sh.scan_c[k];
-      if (ic - c < nth && nth <= ic) {
-        uint32_t left = nth - (ic - c);
-        for (int i = i0; i < i1; ++i)
-          if (r.x[i] == same && --left == 0) {
-            sh.found = i;
-            break;
-          }
-      }
+    for (int u = 0; u < U; ++u) {
+      auto bit = [&](float v, uint32_t one) { return a.has(v) || b.has(v) ? one : 0u; };
+      const uint32_t some = bit(w[u].x, 1u) | bit(w[u].y, 2u) | bit(w[u].z, 4u) | bit(w[u].w, 8u);
+      in |= j0 + u * kSampleThreads < n4 ? some << (4 * u) : 0u;
     }
-    __syncthreads();
-    return;
-  }
-  if (tid == 0) sh.n_list = 0;
-  __syncthreads();
-  r.each(lists, [&](float x, int i) {
-    uint64_t m;
-    if (!mine(x, &m)) return;
-    const uint32_t at = atomicAdd(&sh.n_list, 1u);
-    if (at < kSampleList) sh.key[at] = order_key(x), sh.index[at] = i, sh.weight[at] = m;
-  });
-  __syncthreads();
-  const int have = min(sh.n_list, static_cast<uint32_t>(kSampleList));
-  if (tid < have) {
-    const uint32_t key = sh.key[tid];
-    const int at = sh.index[tid];
-    const uint64_t w = sh.weight[tid];
-    uint64_t m = base_m;
-    uint32_t c = base_c, rank = 0;
-    for (int j = 0; j < have; ++j) {
-      const uint32_t k = sh.key[j];
-      if (k > key || (k == key && sh.index[j] < at)) m += sh.weight[j], ++rank;
-    }
-    c += rank;
-    // the first that is as wanted, or the last
-    const bool ok = there(c + 1, m + w);
-    if ((ok && (rank == 0 || !there(c, m))) || (!ok && static_cast<int>(rank) == have - 1)) {
-      sh.upto = before + static_cast<double>(m + w) * scale;
-      sh.tokens = above + c + 1;
-      sh.own = static_cast<double>(w) * scale;
-      sh.found = at;
+    for (; in; in &= in - 1) {
+      const int k = __ffs(static_cast<int>(in)) - 1, i = head + 4 * (j0 + k / 4 * kSampleThreads) + k % 4;
+      f(x[i], i);
     }
   }
-  __syncthreads();
+}
+
+// A range that holds the logits of bins first .. last, from their edges in t with room for their rounding.
+__device__ __forceinline__ SampleRange range_of(const SampleGrid& grid, int first, int last) {
+  const double lo = (grid.top - last) / grid.per, hi = (grid.top - first + 1.0) / grid.per;
+  return SampleRange{isfinite(lo) ? static_cast<float>(lo - fabs(lo) * 1e-6 - 1e-37) : -INFINITY,
+                     isfinite(hi) ? static_cast<float>(hi + fabs(hi) * 1e-6 + 1e-37) : INFINITY};
 }
 
 __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, int chunks) {
   __shared__ SampleShared sh;
-  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  SampleRow r;
-  r.x = a.logits + static_cast<size_t>(row) * a.ldl;
-  r.chunk = reinterpret_cast<const SampleChunk*>(a.ws) + static_cast<size_t>(row) * chunks;
-  r.vocab = a.vocab, r.chunks = chunks;
-  const SampleChunk& own_chunk = r.chunk[min(lane % kSampleChunks, chunks - 1)];
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, vocab = a.vocab;
+  const float* x = a.logits + static_cast<size_t>(row) * a.ldl;
+  const SampleChunk* chunk = reinterpret_cast<const SampleChunk*>(a.ws) + static_cast<size_t>(row) * chunks;
+  const SampleChunk& own_chunk = chunk[min(lane % kSampleChunks, chunks - 1)];
   SampleBest b{own_chunk.max, own_chunk.index};
   const float chunk_max = b.v;
 #pragma unroll
@@ -417,37 +278,33 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
     }
     return;
   }
-  r.grid = sample_grid(b.v, t);
+  const float min_p = a.min_p ? a.min_p[row] : 0.f, top_p = a.top_p ? a.top_p[row] : 1.f, u = a.u[row];
+  const int top_k = a.top_k ? a.top_k[row] : 0;
+  const SampleGrid grid = sample_grid(b.v, t);
   if (tid < chunks) {
     // (an infinite difference, or that of infinities: all of the chunk or nothing)
-    const double d = chunk_max == b.v ? 0.0 : r.grid.top - sample_grid(chunk_max, t).top;
+    const double d = chunk_max == b.v ? 0.0 : grid.top - sample_grid(chunk_max, t).top;
     const bool any = chunk_max > -INFINITY && d < static_cast<double>(kSampleBins);
     sh.shift[tid] = any ? static_cast<int>(d) : kSampleBins;
     sh.covered[tid] = any ? own_chunk.covered : 0;
   }
-#pragma unroll
-  for (int k = 0; k < SampleRow::L; ++k) {
-    const int at = tid + k * kSampleThreads, c = at / kSampleList;
-    const SampleChunk& from = r.chunk[min(c, chunks - 1)];
-    const bool on = c < chunks && from.max > -INFINITY && at % kSampleList < from.listed;
-    const float2 e = on ? from.list[at % kSampleList] : make_float2(__builtin_nanf(""), 0.f);
-    r.listed[k] = e.x;
-    r.listed_at[k] = __float_as_int(e.y);
-  }
+  if (tid == 0) sh.n = 0, sh.some = 0, sh.some_n = 0;
+  sh.wanted[tid] = 0;
   __syncthreads();
-  // the row's histogram and its running sums
+
+  // The row's histogram and its running sums.
   uint64_t mass = 0;
   uint32_t count = 0;
 #pragma unroll 8
   for (int c = 0; c < chunks; ++c) {
     const int at = tid - sh.shift[c];
-    uint64_t v = r.chunk[c].bin[max(at, 0)];
+    uint64_t v = chunk[c].bin[max(at, 0)];
     v = at < 0 ? 0 : v;
     mass += v & kMassMask;
     count += static_cast<uint32_t>(v >> kMassBits);
   }
-  const double w = static_cast<double>(mass) * bin_scale(tid);
-  double iw = w;
+  const double scale_here = bin_scale(tid);
+  double iw = static_cast<double>(mass) * scale_here;
   uint32_t ic = count;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -455,73 +312,294 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
     const uint32_t pc = __shfl_up(ic, o, kWave);
     if (lane >= o) iw += pw, ic += pc;
   }
-  if (lane == 63) sh.scan_w[wave] = iw, sh.scan_c[wave] = ic;
-  // (the sum before a bin is that of its lower neighbours' lanes, not the sum with it less its own)
+  const uint64_t any = __ballot(count > 0);
+  if (lane == 63) sh.scan_w[wave] = iw, sh.scan_c[wave] = ic, sh.scan_last[wave] = any ? 64 * wave + 63 - __clzll(any) : 0;
   double bw = __shfl_up(iw, 1, kWave);
   if (lane == 0) bw = 0.0;
-  if (tid == 0) sh.bin = 0;
   __syncthreads();
   double head = 0.0;
   uint32_t bc = ic - count;
-  for (int k = 0; k < wave; ++k) head += sh.scan_w[k], bc += sh.scan_c[k];
+  int last_bin = 0;
+#pragma unroll
+  for (int k = 0; k < kSampleThreads / 64; ++k) {
+    head += k < wave ? sh.scan_w[k] : 0.0;
+    bc += k < wave ? sh.scan_c[k] : 0;
+    last_bin = max(last_bin, sh.scan_last[k]);
+  }
+  const double my_with = weight_up_to(head + bw, mass, scale_here);
+  const uint32_t my_tokens = bc + count;
   sh.before[tid] = head + bw;
-  sh.with[tid] = (head + bw) + w;
+  sh.with[tid] = my_with;
   sh.above[tid] = bc;
   sh.count[tid] = count;
-  if (count > 0) atomicMax(&sh.bin, tid);
-  __syncthreads();
-  r.last_bin = sh.bin;
-  double total = sh.with[r.last_bin];
-  uint32_t tokens = sh.above[r.last_bin] + sh.count[r.last_bin];
   __syncthreads();
 
-  const float min_p = a.min_p ? a.min_p[row] : 0.f, top_p = a.top_p ? a.top_p[row] : 1.f;
-  const int top_k = a.top_k ? a.top_k[row] : 0;
+  // The first bin that holds any token and whose count or weight, with the bins above, is as wanted; the last one with a
+  // token where none is.
+  int searches = 0;
+  auto search_bins = [&](SampleWant how, uint32_t n, double want) {
+    int(&found)[kSampleThreads / 64] = sh.found_bin[searches++];
+    const uint64_t ok = __ballot(count > 0 && (how == kByCount ? my_tokens >= n : how == kReach ? my_with >= want : my_with > want));
+    if (lane == 0) found[wave] = ok ? 64 * wave + __ffsll(static_cast<unsigned long long>(ok)) - 1 : last_bin;
+    __syncthreads();
+    int bin = last_bin;
+#pragma unroll
+    for (int k = 0; k < kSampleThreads / 64; ++k) bin = min(bin, found[k]);
+    return bin;
+  };
+
+  // Which bins the searches may end in: each takes the sums at the edges of the bin, or bins, of the one before.
+  double lo = sh.with[last_bin], hi = lo;
+  uint32_t tokens_lo = sh.above[last_bin] + sh.count[last_bin], tokens_hi = tokens_lo;
+  int top_bin = kSampleBins, low_bin = -1;  // the first and the last of those of the filters
+  SampleRange token_range;                  // of the token's
+  auto want_bins = [&](int first, int last) {
+    for (int k = first + tid; k <= last; k += kSampleThreads) sh.wanted[k] = 1;
+    lo = sh.before[first], hi = sh.with[last];
+    tokens_lo = sh.above[first], tokens_hi = sh.above[last] + sh.count[last];
+  };
+  const double least = fmin(static_cast<double>(min_p), 1.0);
+  int min_bin = -1;  // the bin that the least weight falls into
   if (min_p > 0.f) {
-    // the bin that the least weight falls into; its tokens are taken by their weights in fp64
-    const double least = fmin(static_cast<double>(min_p), 1.0), inv = 1.0 / static_cast<double>(t);
-    const double depth = r.grid.top == static_cast<double>(INFINITY)
+    const double depth = grid.top == static_cast<double>(INFINITY)
                              ? 0.0
-                             : r.grid.top - floor(static_cast<double>(b.v) * r.grid.per + 32.0 * log(least));
-    if (depth < static_cast<double>(kSampleBins) && static_cast<int>(depth) <= r.last_bin) {
-      const int bin = static_cast<int>(depth);
-      if (tid == 0) sh.some = 0, sh.some_n = 0;
-      __syncthreads();
-      const bool lists = r.at_hand(sh, bin);
-      uint64_t m_sum = 0;
-      uint32_t n = 0;
-      r.each(lists, [&](float x, int) {
-        uint64_t m;
-        if (sample_bin(r.grid, x, &m) != bin) return;
-        const double e = x == b.v ? 1.0 : exp((static_cast<double>(x) - static_cast<double>(b.v)) * inv);
-        if (e >= least) m_sum += m, ++n;
-      });
-      if (n > 0) {
-        lds_add(&sh.some, m_sum);
-        atomicAdd(&sh.some_n, n);
-      }
-      __syncthreads();
-      total = sh.before[bin] + static_cast<double>(sh.some) * bin_scale(bin);
-      tokens = sh.above[bin] + sh.some_n;
-      __syncthreads();
+                             : grid.top - floor(static_cast<double>(b.v) * grid.per + 32.0 * log(least));
+    if (depth <= static_cast<double>(last_bin)) {
+      min_bin = top_bin = low_bin = static_cast<int>(depth);
+      want_bins(min_bin, min_bin);
     }
   }
-  if (top_k > 0 && static_cast<uint32_t>(top_k) < tokens) {
-    locate(sh, r, kByCount, top_k, 0.0, false);
-    total = sh.upto;
-    __syncthreads();
+  if (top_k > 0 && static_cast<uint32_t>(top_k) < tokens_hi) {
+    const int k = search_bins(kByCount, top_k, 0.0);
+    const uint32_t all = tokens_lo;
+    const double before = lo;
+    want_bins(k, k);
+    top_bin = min(top_bin, k), low_bin = max(low_bin, k);
+    // (in the bin of min_p, which of the two comes first is open)
+    if (k == min_bin && all < static_cast<uint32_t>(top_k)) lo = before, tokens_lo = all;
   }
+  const double share = static_cast<double>(fmaxf(top_p, 0.f));
   if (top_p < 1.f) {
-    locate(sh, r, kReach, 0, static_cast<double>(fmaxf(top_p, 0.f)) * total, false);
-    total = fmin(total, sh.upto);
+    const int first = search_bins(kReach, 0, share * lo), last = search_bins(kReach, 0, share * hi);
+    want_bins(first, last);
+    top_bin = min(top_bin, first), low_bin = max(low_bin, last);
+  }
+  const double part = static_cast<double>(u > 0.f ? u : 0.f);
+  if (u >= 1.f) {
+    const int first = search_bins(kReach, 0, lo), last = search_bins(kReach, 0, hi);
+    want_bins(first, last);
+    token_range = range_of(grid, first, last);
+  } else {
+    const int first = search_bins(kPass, 0, part * lo), last = search_bins(kPass, 0, part * hi);
+    want_bins(first, last);
+    token_range = range_of(grid, first, last);
+  }
+  __syncthreads();
+
+  // Gather them: from the chunks' lists where those hold them all, else from the row.
+  const bool mine_wanted = sh.wanted[tid] != 0;
+  bool listed = true;
+  for (int c = 0; c < chunks; ++c) listed &= !mine_wanted || tid < sh.shift[c] + sh.covered[c];
+  if (mine_wanted && count > 0) atomicAdd(&sh.n, count);
+  const bool lists = __syncthreads_and(listed);
+  const bool gather = sh.n <= kSampleGather;
+  __syncthreads();
+  if (tid == 0) sh.n = 0;
+  __syncthreads();
+  auto take = [&](float v, int i) {
+    uint64_t m;
+    const int at = sample_bin(grid, v, &m);
+    if (at < 0 || !sh.wanted[at]) return;
+    const uint32_t k = atomicAdd(&sh.n, 1u);
+    if (k < kSampleGather) sh.key[k] = order_key(v), sh.index[k] = i, sh.bin[k] = static_cast<uint16_t>(at);
+  };
+  if (gather) {
+    if (lists) {
+#pragma unroll
+      for (int k = 0; k < kSampleChunks * kSampleList / kSampleThreads; ++k) {
+        const int at = tid + k * kSampleThreads, c = at / kSampleList;
+        if (c >= chunks || sh.shift[c] >= kSampleBins || at % kSampleList >= chunk[c].listed) continue;
+        const float2 e = chunk[c].list[at % kSampleList];
+        take(e.x, __float_as_int(e.y));
+      }
+    } else {
+      each_of_row(x, vocab, token_range, low_bin >= 0 ? range_of(grid, top_bin, low_bin) : kNoRange, take);
+    }
+  }
+  __syncthreads();
+  const int held = gather ? min(sh.n, static_cast<uint32_t>(kSampleGather)) : 0;
+
+  double total = sh.with[last_bin];
+  uint32_t tokens = sh.above[last_bin] + sh.count[last_bin];
+  if (min_bin >= 0) {
+    // its tokens are taken by their weights in fp64
+    const double inv = 1.0 / static_cast<double>(t);
+    auto add = [&](float v) {
+      uint64_t m;
+      if (sample_bin(grid, v, &m) != min_bin) return;
+      const double e = v == b.v ? 1.0 : exp((static_cast<double>(v) - static_cast<double>(b.v)) * inv);
+      if (e >= least) {
+        lds_add(&sh.some, m);
+        atomicAdd(&sh.some_n, 1u);
+      }
+    };
+    if (gather) {
+      for (int k = tid; k < held; k += kSampleThreads)
+        if (sh.bin[k] == min_bin) add(key_value(sh.key[k]));
+    } else {
+      each_of_row(x, vocab, range_of(grid, min_bin, min_bin), kNoRange, [&](float v, int) { add(v); });
+    }
+    __syncthreads();
+    total = weight_up_to(sh.before[min_bin], sh.some, bin_scale(min_bin));
+    tokens = sh.above[min_bin] + sh.some_n;
+  }
+
+  // top-k, top-p, the token
+#pragma unroll 1
+  for (int step = 0; step < 3; ++step) {
+    SampleWant how = step == 0 ? kByCount : step == 1 || u >= 1.f ? kReach : kPass;
+    const double want = step == 1 ? share * total : u >= 1.f ? total : part * total;
+    if (step == 0 && !(top_k > 0 && static_cast<uint32_t>(top_k) < tokens)) continue;
+    if (step == 1 && !(top_p < 1.f)) continue;
+    const uint32_t want_n = top_k;
+    const int bin = search_bins(how, want_n, want);
+    const double before = sh.before[bin], scale = bin_scale(bin);
+    const uint32_t above = sh.above[bin];
+    const bool from_row = !gather || !sh.wanted[bin];
+    auto there = [&](uint32_t c, uint64_t m) {
+      const double upto = weight_up_to(before, m, scale);
+      return how == kByCount ? above + c >= want_n : how == kReach ? upto >= want : upto > want;
+    };
+    const SampleRange range = range_of(grid, bin, bin);
+    // f(order key, index, mass) of the bin's tokens
+    auto each = [&](auto f) {
+      if (from_row) {
+        each_of_row(x, vocab, range, kNoRange, [&](float v, int i) {
+          uint64_t m;
+          if (sample_bin(grid, v, &m) == bin) f(order_key(v), i, m);
+        });
+      } else {
+        for (int k = tid; k < held; k += kSampleThreads)
+          if (sh.bin[k] == bin) {
+            uint64_t m = 0;
+            sample_bin(grid, key_value(sh.key[k]), &m);
+            f(sh.key[k], sh.index[k], m);
+          }
+      }
+    };
+    uint64_t base_m = 0;  // of the bin's tokens above those of [klo, khi], order keys
+    uint32_t base_c = 0, n = sh.count[bin], klo = order_key(range.lo), khi = order_key(range.hi);
+    while (n > kSampleRank && klo < khi) {
+      const int shift = max(0, 32 - __clz(khi - klo) - 10);  // (khi - klo) >> shift < 1024
+      sh.sub_mass[tid] = 0, sh.sub_count[tid] = 0;
+      if (tid == 0) sh.sub = -1, sh.first = kSampleBins;
+      __syncthreads();
+      each([&](uint32_t k, int, uint64_t m) {
+        if (k < klo || k > khi) return;
+        const uint32_t s = (khi - k) >> shift;
+        lds_add(&sh.sub_mass[s], m);
+        atomicAdd(&sh.sub_count[s], 1u);
+      });
+      __syncthreads();
+      const uint64_t m = sh.sub_mass[tid];
+      const uint32_t c = sh.sub_count[tid];
+      uint64_t im = m;
+      uint32_t jc = c;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint64_t pm = __shfl_up(static_cast<unsigned long long>(im), o, kWave);
+        const uint32_t pc = __shfl_up(jc, o, kWave);
+        if (lane >= o) im += pm, jc += pc;
+      }
+      if (lane == 63) sh.scan_m[wave] = im, sh.scan_c[wave] = jc;
+      __syncthreads();
+      im += base_m, jc += base_c;
+      for (int k = 0; k < wave; ++k) im += sh.scan_m[k], jc += sh.scan_c[k];
+      // the first that is as wanted, or the last that holds any
+      if (c > 0) atomicMax(&sh.sub, tid);
+      if (c > 0 && there(jc, im)) atomicMin(&sh.first, tid);
+      __syncthreads();
+      const int sub = sh.first < kSampleBins ? sh.first : sh.sub;
+      if (tid == sub) sh.some = im - m, sh.some_n = jc - c, sh.n = c;
+      __syncthreads();
+      base_m = sh.some, base_c = sh.some_n, n = sh.n;
+      const uint64_t top = khi, from = (static_cast<uint64_t>(sub) + 1) << shift;
+      klo = top + 1 > from ? max(klo, static_cast<uint32_t>(top + 1 - from)) : klo;
+      khi = static_cast<uint32_t>(top - (static_cast<uint64_t>(sub) << shift));
+      __syncthreads();
+    }
+    if (n > kSampleRank) {  // all the same
+      uint64_t m1;
+      sample_bin(grid, key_value(khi), &m1);
+      uint32_t nth = 1;  // the least that is as wanted, by halves: `there` only ever turns true
+      for (uint32_t l = 1, h = n; l < h;) {
+        const uint32_t mid = l + (h - l) / 2;
+        if (there(base_c + mid, base_m + mid * m1)) h = mid;
+        else l = mid + 1;
+        nth = l;
+      }
+      if (tid == 0) {
+        sh.upto = weight_up_to(before, base_m + nth * m1, scale);
+        sh.own = static_cast<double>(m1) * scale;
+      }
+      if (step == 2) {
+        const int span = (vocab + kSampleThreads - 1) / kSampleThreads, i0 = tid * span, i1 = min(i0 + span, vocab);
+        const float same = key_value(khi);
+        uint32_t c = 0;
+        for (int i = i0; i < i1; ++i) c += x[i] == same ? 1 : 0;
+        uint32_t jc = c;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const uint32_t pc = __shfl_up(jc, o, kWave);
+          if (lane >= o) jc += pc;
+        }
+        if (lane == 63) sh.scan_c[wave] = jc;
+        __syncthreads();
+        for (int k = 0; k < wave; ++k) jc += sh.scan_c[k];
+        if (jc - c < nth && nth <= jc) {
+          uint32_t left = nth - (jc - c);
+          for (int i = i0; i < i1; ++i)
+            if (x[i] == same && --left == 0) {
+              sh.found = i;
+              break;
+            }
+        }
+      }
+    } else {
+      if (tid == 0) sh.n = 0;
+      __syncthreads();
+      each([&](uint32_t k, int i, uint64_t m) {
+        if (k < klo || k > khi) return;
+        const uint32_t at = atomicAdd(&sh.n, 1u);
+        if (at < kSampleRank) sh.rank_key[at] = k, sh.rank_index[at] = i, sh.rank_mass[at] = m;
+      });
+      __syncthreads();
+      const int have = min(sh.n, static_cast<uint32_t>(kSampleRank));
+      if (tid < have) {
+        const uint32_t key = sh.rank_key[tid];
+        const int at = sh.rank_index[tid];
+        const uint64_t own = sh.rank_mass[tid];
+        uint64_t m = base_m;
+        uint32_t rank = 0;
+        for (int j = 0; j < have; ++j) {
+          const uint32_t k = sh.rank_key[j];
+          const bool higher = k > key || (k == key && sh.rank_index[j] < at);
+          m += higher ? sh.rank_mass[j] : 0;
+          rank += higher ? 1 : 0;
+        }
+        // the first that is as wanted, or the last
+        const bool ok = there(base_c + rank + 1, m + own);
+        if (ok ? rank == 0 || !there(base_c + rank, m) : static_cast<int>(rank) == have - 1) {
+          sh.upto = weight_up_to(before, m + own, scale);
+          sh.own = static_cast<double>(own) * scale;
+          sh.found = at;
+        }
+      }
+    }
+    __syncthreads();
+    if (step < 2) total = fmin(total, sh.upto);
     __syncthreads();
   }
-  // u from 1 on: the last kept token, the first whose sum reaches all of it
-  const float u = a.u[row];
-  if (u >= 1.f)
-    locate(sh, r, kReach, 0, total, true);
-  else
-    locate(sh, r, kPass, 0, static_cast<double>(u > 0.f ? u : 0.f) * total, true);
   if (tid == 0) {
     a.out[row] = sh.found;
     if (a.prob) a.prob[row] = static_cast<float>(sh.own / total);
