@@ -12,61 +12,180 @@ namespace metro {
 //   y <- y / sqrt(mean(y^2) + eps) * g,
 // then turned by pairs (i, i + hd/2) with the position's (cos, sin):
 //   (a, b) -> (a c - b s, a s + b c),
-// all in fp32, and rounded to bf16 once.  v is rounded as it is.  One wave per
-// (row, head); lane j < hd/2 takes the pair (j, j + hd/2).
+// all in fp32, and rounded to bf16 once.  v is rounded as it is.
+//
+// A wave takes RW = 8 (16 for head dim 64) rows; a lane has 8 pairs of one row,
+// with their cosines and sines in registers for all heads that the wave goes
+// through, the next head's values on their way.  Queries and keys leave as 16-byte
+// stores (a K tile's chunk is 8 dims of one key, those of consecutive keys lie side
+// by side).  A V^T tile holds 4 keys of a dim together, so values are taken four
+// rows at a time where the rows' slots are four such keys, whatever row they begin
+// at, and one by one elsewhere.
 // ---------------------------------------------------------------------------
 template <bool F32>
-__global__ __launch_bounds__(64) void rope_append_kernel(AppendArgs a) {
-  const int nh = a.nq + 2 * a.nkv, hd = a.hd, half = hd / 2;
-  const int t = blockIdx.x / nh, head = blockIdx.x % nh;
-  const int j = threadIdx.x;
-  const bool on = j < half;
-  const size_t at = static_cast<size_t>(t) * a.ld + head * hd;
-  float x = 0.f, y = 0.f;
-  if (on) {
-    x = F32 ? a.y32[at + j] : bf16_to_f32(a.y16[at + j]);
-    y = F32 ? a.y32[at + j + half] : bf16_to_f32(a.y16[at + j + half]);
+__device__ __forceinline__ void load8(const AppendArgs& a, size_t at, float (&x)[8]) {
+  if constexpr (F32) {
+    const float4 u = *reinterpret_cast<const float4*>(a.y32 + at), v = *reinterpret_cast<const float4*>(a.y32 + at + 4);
+    x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+  } else {
+    const uint4 u = *reinterpret_cast<const uint4*>(a.y16 + at);
+    x[0] = lo_bf16(u.x), x[1] = hi_bf16(u.x), x[2] = lo_bf16(u.y), x[3] = hi_bf16(u.y);
+    x[4] = lo_bf16(u.z), x[5] = hi_bf16(u.z), x[6] = lo_bf16(u.w), x[7] = hi_bf16(u.w);
   }
-  const int sl = a.slot[t];
-  const bool cached = sl >= 0 && sl / kPage < a.n_pages;
-  if (head >= a.nq + a.nkv) {
-    if (!cached || !on) return;
-    uint16_t* vt = a.kv + kv_offset(sl / kPage, 1, a.nkv, head - a.nq - a.nkv, 0, hd, 0);
-    vt[vt_tile_offset(j, sl % kPage)] = f32_to_bf16(x);
-    vt[vt_tile_offset(j + half, sl % kPage)] = f32_to_bf16(y);
-    return;
-  }
-  const uint16_t* gain = head < a.nq ? a.q_gain : a.k_gain;
-  if (gain) {
-    const float inv = rsqrtf(wave_sum(x * x + y * y) / static_cast<float>(hd) + a.eps);
-    if (on) {
-      x = x * inv * bf16_to_f32(gain[j]);
-      y = y * inv * bf16_to_f32(gain[j + half]);
+}
+
+template <bool F32>
+__device__ __forceinline__ float4 load4(const AppendArgs& a, size_t at) {
+  if constexpr (F32) return *reinterpret_cast<const float4*>(a.y32 + at);
+  const uint2 u = *reinterpret_cast<const uint2*>(a.y16 + at);
+  return make_float4(lo_bf16(u.x), hi_bf16(u.x), lo_bf16(u.y), hi_bf16(u.y));
+}
+
+__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
+  return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+}
+
+__device__ __forceinline__ void times8(float (&x)[8], float s, uint4 g) {
+  x[0] *= s * lo_bf16(g.x), x[1] *= s * hi_bf16(g.x), x[2] *= s * lo_bf16(g.y), x[3] *= s * hi_bf16(g.y);
+  x[4] *= s * lo_bf16(g.z), x[5] *= s * hi_bf16(g.z), x[6] *= s * lo_bf16(g.w), x[7] *= s * hi_bf16(g.w);
+}
+
+template <int HD, bool F32>
+__global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs a, int slices) {
+  constexpr int HALF = HD / 2, LPR = HALF / 8, RW = 64 / LPR;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t0 = blockIdx.x / slices * RW, first = blockIdx.x % slices * 4 + wave, step = 4 * slices;
+  const int n_slots = a.n_pages * kPage, turned = a.nq + a.nkv, heads = turned + a.nkv;
+
+  int h = first;
+  if (h < turned) {
+    const int t = t0 + lane / LPR, d = lane % LPR * 8;
+    const bool on = t < a.T;
+    const int row = on ? t : a.T - 1;
+    const size_t at = static_cast<size_t>(row) * a.ld + d;
+    float x[8], y[8];
+    load8<F32>(a, at + static_cast<size_t>(h) * HD, x);
+    load8<F32>(a, at + static_cast<size_t>(h) * HD + HALF, y);
+    const int p = a.pos[row], slot = a.slot[row];
+    const bool cached = on && slot >= 0 && slot < n_slots;
+    float c[8], s[8];
+    const float4* cs = reinterpret_cast<const float4*>(a.rope + static_cast<size_t>(min(max(p, 0), a.n_pos - 1)) * HALF + d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 v = cs[i];
+      c[2 * i] = v.x, s[2 * i] = v.y, c[2 * i + 1] = v.z, s[2 * i + 1] = v.w;
+    }
+    if (p < 0 || p >= a.n_pos)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) c[i] = s[i] = __builtin_nanf("");
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    const uint4 qg0 = a.q_gain ? *reinterpret_cast<const uint4*>(a.q_gain + d) : none;
+    const uint4 qg1 = a.q_gain ? *reinterpret_cast<const uint4*>(a.q_gain + d + HALF) : none;
+    const uint4 kg0 = a.k_gain ? *reinterpret_cast<const uint4*>(a.k_gain + d) : none;
+    const uint4 kg1 = a.k_gain ? *reinterpret_cast<const uint4*>(a.k_gain + d + HALF) : none;
+    uint16_t* ktile = a.kv + kv_offset(cached ? slot / kPage : 0, 0, a.nkv, 0, 0, HD, 0) + (d / 8 * kPage + (cached ? slot % kPage : 0)) * 8;
+    uint16_t* qrow = a.q + static_cast<size_t>(row) * a.nq * HD + d;
+    for (; h < turned; h += step) {
+      float nx[8], ny[8];
+      const int hn = min(h + step, turned - 1);
+      load8<F32>(a, at + static_cast<size_t>(hn) * HD, nx);
+      load8<F32>(a, at + static_cast<size_t>(hn) * HD + HALF, ny);
+      const bool is_q = h < a.nq;
+      if (is_q ? a.q_gain != nullptr : a.k_gain != nullptr) {
+        float ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss += x[i] * x[i] + y[i] * y[i];
+#pragma unroll
+        for (int o = 1; o < LPR; o <<= 1) ss += __shfl_xor(ss, o, kWave);
+        const float inv = rsqrtf(ss * (1.f / HD) + a.eps);
+        times8(x, inv, is_q ? qg0 : kg0);
+        times8(y, inv, is_q ? qg1 : kg1);
+      }
+      float u[8], v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        u[i] = x[i] * c[i] - y[i] * s[i];
+        v[i] = x[i] * s[i] + y[i] * c[i];
+      }
+      if (is_q) {
+        if (on) {
+          *reinterpret_cast<uint4*>(qrow + h * HD) = pack8(u);
+          *reinterpret_cast<uint4*>(qrow + h * HD + HALF) = pack8(v);
+        }
+      } else if (cached) {
+        uint16_t* k = ktile + static_cast<size_t>(h - a.nq) * kPage * HD;
+        *reinterpret_cast<uint4*>(k) = pack8(u);
+        *reinterpret_cast<uint4*>(k + HALF / 8 * kPage * 8) = pack8(v);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = nx[i], y[i] = ny[i];
     }
   }
-  if (!on) return;
-  const int p = a.pos[t];
-  const float nan = __builtin_nanf("");
-  const float2 c = p >= 0 && p < a.n_pos ? a.rope[static_cast<size_t>(p) * half + j] : make_float2(nan, nan);
-  const uint16_t ra = f32_to_bf16(x * c.x - y * c.y), rb = f32_to_bf16(x * c.y + y * c.x);
-  if (head < a.nq) {
-    uint16_t* dst = a.q + (static_cast<size_t>(t) * a.nq + head) * hd;
-    dst[j] = ra;
-    dst[j + half] = rb;
-  } else if (cached) {
-    uint16_t* kt = a.kv + kv_offset(sl / kPage, 0, a.nkv, head - a.nq, 0, hd, 0);
-    kt[k_tile_offset(sl % kPage, j)] = ra;
-    kt[k_tile_offset(sl % kPage, j + half)] = rb;
+  if (h >= heads) return;
+
+  // Which rows begin four keys of a tile that follow one another (lane i: row t0 - 3 + i; the first three rows may be
+  // taken along by such a one before them).
+  bool leads = false;
+  bool stored = false;
+  if (const int t = t0 - 3 + lane; lane < RW + 3 && t >= 0 && t < a.T) {
+    const int s0 = a.slot[t];
+    stored = s0 >= 0 && s0 < n_slots;
+    if (stored && s0 % 4 == 0 && t + 3 < a.T) leads = a.slot[t + 1] == s0 + 1 && a.slot[t + 2] == s0 + 2 && a.slot[t + 3] == s0 + 3;
+  }
+  const uint64_t lead = __ballot(leads);
+  const uint64_t own = lead >> 3, taken = (lead | lead << 1 | lead << 2 | lead << 3) >> 3;
+  const uint32_t alone = static_cast<uint32_t>((__ballot(stored) >> 3) & ~taken) & ((1u << RW) - 1);
+  constexpr int LPV = HD / 4;  // lanes of a row of values, four dims each
+  const int d = lane % LPV * 4;
+  // this lane's quad: the (lane / LPV)-th of the wave's (at most RW / 4 begin within RW rows)
+  uint32_t bits = static_cast<uint32_t>(own) & ((1u << RW) - 1);
+  for (int k = 0; k < lane / LPV; ++k) bits &= bits - 1;
+  const bool quad = bits != 0;
+  const int tq = t0 + (quad ? __ffs(static_cast<int>(bits)) - 1 : 0);
+  for (; h < heads; h += step) {
+    const int head = h - turned;
+    if (quad) {
+      const size_t at = static_cast<size_t>(tq) * a.ld + static_cast<size_t>(h) * HD + d;
+      const float4 r0 = load4<F32>(a, at), r1 = load4<F32>(a, at + a.ld), r2 = load4<F32>(a, at + 2 * static_cast<size_t>(a.ld)),
+                   r3 = load4<F32>(a, at + 3 * static_cast<size_t>(a.ld));
+      const int slot = a.slot[tq];
+      uint16_t* vt = a.kv + kv_offset(slot / kPage, 1, a.nkv, head, 0, HD, 0) + vt_tile_offset(d, slot % kPage);
+      *reinterpret_cast<uint2*>(vt) = make_uint2(pack_bf16x2(r0.x, r1.x), pack_bf16x2(r2.x, r3.x));
+      *reinterpret_cast<uint2*>(vt + 8) = make_uint2(pack_bf16x2(r0.y, r1.y), pack_bf16x2(r2.y, r3.y));
+      *reinterpret_cast<uint2*>(vt + 16) = make_uint2(pack_bf16x2(r0.z, r1.z), pack_bf16x2(r2.z, r3.z));
+      *reinterpret_cast<uint2*>(vt + 24) = make_uint2(pack_bf16x2(r0.w, r1.w), pack_bf16x2(r2.w, r3.w));
+    }
+    // one by one: each LPV lanes take another of these rows
+    uint32_t rest = alone;
+    for (int k = 0; k < lane / LPV; ++k) rest &= rest - 1;
+    while (rest) {
+      const int t = t0 + __ffs(static_cast<int>(rest)) - 1, slot = a.slot[t];
+      const float4 r = load4<F32>(a, static_cast<size_t>(t) * a.ld + static_cast<size_t>(h) * HD + d);
+      uint16_t* vt = a.kv + kv_offset(slot / kPage, 1, a.nkv, head, 0, HD, 0) + vt_tile_offset(d, slot % kPage);
+      vt[0] = f32_to_bf16(r.x);
+      vt[8] = f32_to_bf16(r.y);
+      vt[16] = f32_to_bf16(r.z);
+      vt[24] = f32_to_bf16(r.w);
+      for (int k = 0; k < 64 / LPV; ++k) rest &= rest - 1;
+    }
   }
 }
 
 hipError_t launch_rope_append(const AppendArgs& a, hipStream_t s) {
   if (a.T <= 0) return hipSuccess;
-  const dim3 grid(a.T * (a.nq + 2 * a.nkv));
-  if (a.y32)
-    launch_kernel(rope_append_kernel<true>, grid, dim3(64), 0, s, a);
-  else
-    launch_kernel(rope_append_kernel<false>, grid, dim3(64), 0, s, a);
+  const int rows = a.hd == 128 ? 8 : 16, blocks = (a.T + rows - 1) / rows, heads = a.nq + 2 * a.nkv;
+  // few rows: their heads over more workgroups, down to one a wave
+  int slices = 1;
+  while (slices < (heads + 3) / 4 && static_cast<int64_t>(blocks) * slices < 1024) ++slices;
+  const dim3 grid(blocks * slices);
+  if (a.hd == 128) {
+    if (a.y32) launch_kernel((rope_append_kernel<128, true>), grid, dim3(256), 0, s, a, slices);
+    else launch_kernel((rope_append_kernel<128, false>), grid, dim3(256), 0, s, a, slices);
+  } else {
+    if (a.y32) launch_kernel((rope_append_kernel<64, true>), grid, dim3(256), 0, s, a, slices);
+    else launch_kernel((rope_append_kernel<64, false>), grid, dim3(256), 0, s, a, slices);
+  }
   return hipGetLastError();
 }
 
