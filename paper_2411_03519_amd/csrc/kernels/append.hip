@@ -196,43 +196,49 @@ hipError_t launch_rope_append(const AppendArgs& a, hipStream_t s) {
 // in the list's order, so no other thread can come between and no barrier is
 // needed.  Grid: (chunks of a layer's heads, layers, groups).
 // ---------------------------------------------------------------------------
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 template <bool V>
-__device__ __forceinline__ void move_chunk(const MoveArgs& a, uint16_t* base, int unit, int lo, int hi) {
-  const int per_head = V ? a.hd / 2 : a.hd / 8;  // chunks of a key in a tile
-  const int h = unit / per_head, c = unit % per_head;
+__device__ __forceinline__ void move_run(const MoveArgs& a, uint16_t* layer, uint32_t own, int lo, int n) {
   const int slots = a.n_pages * kPage;
-  auto where = [&](int slot) {
-    const int key = slot % kPage;
-    const int in = V ? (((c >> 4) * 4 + (key >> 2)) * 16 + (c & 15)) * 8 + (key & 3) : (c * 16 + key) * 8;
-    return base + kv_offset(slot / kPage, V ? 1 : 0, a.nkv, h, 0, a.hd, 0) + in;
+  const size_t page = static_cast<size_t>(2) * a.nkv * kPage * a.hd;
+  // own: the thread's chunk in a page; the key's place in it is the same for all threads
+  auto where = [&](int slot) __attribute__((always_inline)) {
+    const uint32_t key = static_cast<uint32_t>(slot) % kPage;
+    return layer + (static_cast<uint32_t>(slot) / kPage * page + (V ? key / 4 * 128 + key % 4 : key * 8)) + own;
   };
-  for (int m0 = lo; m0 < hi; m0 += kMoveRun) {
-    const int n = min(kMoveRun, hi - m0);
-    uint4 k[V ? 1 : kMoveRun];
-    uint32_t v[V ? kMoveRun : 1];
+  u32x4 k[V ? 1 : kMoveRun];
+  uint32_t v[V ? kMoveRun : 1];
 #pragma unroll
-    for (int m = 0; m < kMoveRun; ++m) {
-      if (m >= n) continue;
-      const int s = min(max(a.src[m0 + m], 0), slots - 1);
-      if constexpr (V)
-        v[m] = where(s)[0] | (static_cast<uint32_t>(where(s)[4]) << 16);
-      else
-        k[m] = *reinterpret_cast<const uint4*>(where(s));
+  for (int m = 0; m < kMoveRun; ++m)
+    if (m < n) {
+      const uint16_t* from = where(min(max(a.src[lo + m], 0), slots - 1));
+      if constexpr (V) v[m] = from[0] | (static_cast<uint32_t>(from[4]) << 16);
+      else k[m] = *reinterpret_cast<const u32x4*>(from);
     }
 #pragma unroll
-    for (int m = 0; m < kMoveRun; ++m) {
-      if (m >= n) continue;
-      const int s = a.src[m0 + m], d = a.dst[m0 + m];
-      if (s == d || s < 0 || s >= slots || d < 0 || d >= slots) continue;
-      uint16_t* to = where(d);
-      if constexpr (V) {
-        to[0] = static_cast<uint16_t>(v[m]);
-        to[4] = static_cast<uint16_t>(v[m] >> 16);
-      } else {
-        *reinterpret_cast<uint4*>(to) = k[m];
+  for (int m = 0; m < kMoveRun; ++m)
+    if (m < n) {
+      const int s = a.src[lo + m], d = a.dst[lo + m];
+      if (s != d && s >= 0 && s < slots && d >= 0 && d < slots) {
+        uint16_t* to = where(d);
+        if constexpr (V) {
+          to[0] = static_cast<uint16_t>(v[m]);
+          to[4] = static_cast<uint16_t>(v[m] >> 16);
+        } else {
+          *reinterpret_cast<u32x4*>(to) = k[m];
+        }
       }
     }
-  }
+}
+
+template <bool V>
+__device__ __forceinline__ void move_chunk(const MoveArgs& a, uint16_t* layer, int unit, int lo, int hi) {
+  const int per_head = V ? a.hd / 2 : a.hd / 8;  // chunks of a key in a tile; one of V^T holds dims d and d + 16 of four keys
+  const uint32_t h = unit / per_head, c = unit % per_head;
+  const uint32_t own = ((V ? a.nkv : 0) + h) * kPage * a.hd + (V ? c / 16 * 512 + c % 16 * 8 : c * 128);
+#pragma unroll 1
+  for (int m = lo; m < hi; m += kMoveRun) move_run<V>(a, layer, own, m, min(kMoveRun, hi - m));
 }
 
 __global__ __launch_bounds__(128) void kv_move_kernel(MoveArgs a) {

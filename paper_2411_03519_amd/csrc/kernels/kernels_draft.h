@@ -33,7 +33,7 @@ struct MoveArgs {
   int layers, n_pages, nkv, hd, groups, moves;
 };
 constexpr int kMoveMaxGroups = 65535, kMoveMaxLayers = 65535;
-constexpr int kMoveRun = 32;  // moves of a group that are read before any of them is written
+constexpr int kMoveRun = 8;  // moves of a group that are read before any of them is written
 hipError_t launch_kv_move(const MoveArgs& a, hipStream_t s);
 
 // --- attention of drafted trees (attn_tree.hip) -------------------------------
