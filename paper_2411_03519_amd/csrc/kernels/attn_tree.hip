@@ -532,8 +532,8 @@ __global__ __launch_bounds__(kTreeSharedWaves * 64, 4) void attn_tree_shared_ker
     tree_shared_wave<HD, false>(a, w, ring, wave, lane, splits, gl);
 }
 
-// The splits of the items that have several, a workgroup for each query, a wave for each head in turn: lane l brings split
-// l's maximum and sum, then each HD / 4 lanes add up the outputs of every PER-th split (four values a lane), and those
+// The splits of the items that have several, a workgroup for four heads of a query, a wave for each: lane l brings split l's
+// maximum and sum, then each HD / 4 lanes add up the outputs of every PER-th split (four values a lane), and those
 // sums are added in order.
 template <int HD>
 __global__ __launch_bounds__(256) void attn_tree_combine_kernel(TreeArgs a, int splits, int pairs_per_split) {
@@ -544,7 +544,7 @@ __global__ __launch_bounds__(256) void attn_tree_combine_kernel(TreeArgs a, int 
   const int ns = (it.pairs + pairs_per_split - 1) / pairs_per_split;
   if (tok >= it.n || ns <= 1) return;
   const size_t heads = static_cast<size_t>(a.rows) * a.nq;
-  for (int j = blockIdx.y * 4 + wave; j < a.nq; j += 4 * gridDim.y) {
+  if (const int j = blockIdx.y * 4 + wave; j < a.nq) {
     const size_t head = static_cast<size_t>(it.row0 + tok) * a.nq + j;
     const float2 mine = reinterpret_cast<const float2*>(a.part + splits * heads * HD)[min(lane, ns - 1) * heads + head];
     const float M = wave_max(mine.x);
@@ -570,12 +570,54 @@ __global__ __launch_bounds__(256) void attn_tree_combine_kernel(TreeArgs a, int 
       o.z += __shfl_xor(o.z, x, kWave);
       o.w += __shfl_xor(o.w, x, kWave);
     }
-    if (lane >= LN) continue;
+    if (lane >= LN) return;
     const float inv = L == 0.f ? 0.f : 1.f / L;
     uint2 w;
     w.x = pack_bf16x2(o.x * inv, o.y * inv);
     w.y = pack_bf16x2(o.z * inv, o.w * inv);
     *reinterpret_cast<uint2*>(a.out + head * HD + 4 * lane) = w;
+  }
+}
+
+// The same for many queries of few splits: a workgroup for each query, a thread for 16 values of a head, so that one
+// round of loads serves all heads.
+template <int HD>
+__global__ __launch_bounds__(256) void attn_tree_combine_many_kernel(TreeArgs a, int splits, int pairs_per_split) {
+  constexpr int PH = HD / 16;  // threads of a head
+  const int item = blockIdx.x % a.items, tok = blockIdx.x / a.items;
+  const TreeItem it = tree_item(a, item);
+  const int ns = (it.pairs + pairs_per_split - 1) / pairs_per_split;
+  if (tok >= it.n || ns <= 1) return;
+  const size_t heads = static_cast<size_t>(a.rows) * a.nq;
+  for (int unit = threadIdx.x; unit < a.nq * PH; unit += 256) {
+    const size_t head = static_cast<size_t>(it.row0 + tok) * a.nq + unit / PH;
+    const float2* ml = reinterpret_cast<const float2*>(a.part + splits * heads * HD) + head;
+    const float4* po = reinterpret_cast<const float4*>(a.part + head * HD) + unit % PH * 4;
+    float M = kTreeNone;
+#pragma unroll 4
+    for (int s = 0; s < ns; ++s) M = fmaxf(M, ml[s * heads].x);
+    float L = 0.f;
+    float4 o[4] = {};
+#pragma unroll 2
+    for (int s = 0; s < ns; ++s) {
+      const float2 v = ml[s * heads];
+      const float f = exp2f(v.x - M);
+      L += v.y * f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 w = po[s * heads * (HD / 4) + i];
+        o[i].x += w.x * f;
+        o[i].y += w.y * f;
+        o[i].z += w.z * f;
+        o[i].w += w.w * f;
+      }
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    uint4* out = reinterpret_cast<uint4*>(a.out + head * HD + unit % PH * 16);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      out[i] = make_uint4(pack_bf16x2(o[2 * i].x * inv, o[2 * i].y * inv), pack_bf16x2(o[2 * i].z * inv, o[2 * i].w * inv),
+                          pack_bf16x2(o[2 * i + 1].x * inv, o[2 * i + 1].y * inv), pack_bf16x2(o[2 * i + 1].z * inv, o[2 * i + 1].w * inv));
   }
 }
 
@@ -614,11 +656,15 @@ static hipError_t launch_tree_hd(const TreeArgs& a, const TreePlan& p, hipStream
     launch_kernel((attn_tree_kernel<HD, 2>), grid, dim3(kTreeWaves * 64), 0, s, a, p.tiles, p.splits, p.pairs, gl);
   else
     launch_kernel((attn_tree_shared_kernel<HD>), grid, dim3(kTreeSharedWaves * 64), 0, s, a, p.tiles, p.splits, p.pairs, gl);
-  // a head a wave while that leaves at most 4096 workgroups
-  int nb = (a.nq + 3) / 4;
-  while (nb > 1 && static_cast<int64_t>(a.items) * a.max_q * nb > 4096) nb = (nb + 1) / 2;
-  if (p.splits > 1)
-    launch_kernel((attn_tree_combine_kernel<HD>), dim3(a.items * a.max_q, nb), dim3(256), 0, s, a, p.splits, p.pairs);
+  if (p.splits > 1) {
+    // a head a wave while that leaves at most 4096 workgroups
+    const int64_t queries = static_cast<int64_t>(a.items) * a.max_q;
+    const int nb = (a.nq + 3) / 4;
+    if (queries * nb <= 4096)
+      launch_kernel((attn_tree_combine_kernel<HD>), dim3(queries, nb), dim3(256), 0, s, a, p.splits, p.pairs);
+    else
+      launch_kernel((attn_tree_combine_many_kernel<HD>), dim3(queries), dim3(256), 0, s, a, p.splits, p.pairs);
+  }
   return hipGetLastError();
 }
 
