@@ -7,8 +7,8 @@
 // weights that are left.  All three leave a beginning of the order, so the steps
 // need nothing but searches of the running sums of weights and of counts.
 //
-// A search goes by a histogram.  Bins are the whole numbers of t = 32 x / T, the
-// same for every part of a row, counted down from the row's largest; 1024 of them
+// A search goes by a histogram.  Bins lie about the whole numbers of t = 32 x / T,
+// the same for every part of a row, counted down from the row's largest; 1024 of them
 // hold all weights above e^-32 of the largest, the others count as none.  Within
 // its bin a weight is held relative to the bin's upper edge, exp(-g), 0 < g <=
 // 1/32, as a whole multiple of 2^-34: so its relative error is the same 2^-35
@@ -59,36 +59,62 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-// The bins' grid: t = x * per; top is the bin of the largest logit (infinite with it).
+// The bins' grid: t = x * per, bins about its whole numbers; top is the bin of the largest logit (infinite with it).  From
+// 2^50 on, where other logits than the largest lie further than all bins below it, bins have no width.
 struct SampleGrid {
-  double per, top;
+  double per, top, step;
 };
+
+// The nearest whole number of |t| < 2^51, ties to even; the adding leaves no room behind the point.
+__device__ __forceinline__ double nearest_whole(double t) { return (t + 6755399441055744.0) - 6755399441055744.0; }
 
 __device__ __forceinline__ SampleGrid sample_grid(float max, float t) {
   SampleGrid g;
   g.per = 32.0 / static_cast<double>(t);
-  g.top = max == INFINITY ? static_cast<double>(INFINITY) : floor(static_cast<double>(max) * g.per);
+  g.top = max == INFINITY ? static_cast<double>(INFINITY) : nearest_whole(static_cast<double>(max) * g.per);
+  g.step = fabs(g.top) < 1125899906842624.0 ? 1.0 / 32.0 : 0.0;
   return g;
 }
 
-// Bin of a logit below the top one, or -1 where its weight counts as none; *mass: its weight relative to the bin's upper
-// edge in units of 2^-34.  The adding of 2^18 leaves 34 bits behind the point in a double's mantissa, rounded to nearest.
-__device__ __forceinline__ int sample_bin(const SampleGrid& grid, float x, uint64_t* mass) {
-  if (grid.top == static_cast<double>(INFINITY)) {
-    *mass = 1ull << 34;
-    return x == INFINITY ? 0 : -1;
-  }
-  const double t = static_cast<double>(x) * grid.per, whole = floor(t);
-  const double below = grid.top - whole;
-  if (!(below < static_cast<double>(kSampleBins))) return -1;  // (NaN and -inf too)
-  const double g = (t - whole - 1.0) * (1.0 / 32.0);           // -1/32 .. 0; the next term of the series is below 2^-39
+// How many bins a logit lies below the top one (not below 1024, or NaN, where its weight counts as none), for a finite
+// top; *mass: its weight relative to the bin's upper edge, exp(g), in units of 2^-34.  The adding of 2^18 leaves 34 bits
+// behind the point in a double's mantissa.
+__device__ __forceinline__ double bins_below(const SampleGrid& grid, float x, uint64_t* mass) {
+  const double t = static_cast<double>(x) * grid.per, whole = nearest_whole(t);
+  const double g = fma(t - whole, grid.step, -0.5 * grid.step);  // -1/32 .. 0; the series' next term is below 2^-39
   double e = fma(g, 1.0 / 120.0, 1.0 / 24.0);
   e = fma(e, g, 1.0 / 6.0);
   e = fma(e, g, 0.5);
   e = fma(e, g, 1.0);
   e = fma(e, g, 1.0);
   *mass = __double_as_longlong(e + 262144.0) & ((1ull << 52) - 1);
-  return static_cast<int>(below);
+  return grid.top - whole;
+}
+
+// A whole number below 2^31 of a double: the adding of 2^52 leaves it in the lower bits (conversions of fp64 run at a
+// quarter of the rate).
+__device__ __forceinline__ int whole_bits(double d) { return static_cast<int>(__double_as_longlong(d + 4503599627370496.0)); }
+
+// Bin of a logit below the top one, or -1 where its weight counts as none.
+__device__ __forceinline__ int sample_bin(const SampleGrid& grid, float x, uint64_t* mass) {
+  if (grid.top == static_cast<double>(INFINITY)) {
+    *mass = 1ull << 34;
+    return x == INFINITY ? 0 : -1;
+  }
+  const double below = bins_below(grid, x, mass);
+  return below < static_cast<double>(kSampleBins) ? whole_bits(below) : -1;  // (NaN and -inf: -1)
+}
+
+struct SampleRange {
+  float lo, hi;
+  __device__ __forceinline__ bool has(float v) const { return v >= lo && v <= hi; }
+};
+
+// A range that holds the logits of bins first .. last, from their edges in t with room for their rounding.
+__device__ __forceinline__ SampleRange range_of(const SampleGrid& grid, double first, double last) {
+  const double lo = (grid.top - last - 0.5) / grid.per, hi = (grid.top - first + 0.5) / grid.per;
+  return SampleRange{isfinite(lo) ? static_cast<float>(lo - fabs(lo) * 1e-6 - 1e-37) : -INFINITY,
+                     isfinite(hi) ? static_cast<float>(hi + fabs(hi) * 1e-6 + 1e-37) : INFINITY};
 }
 
 struct SampleBest {
@@ -130,24 +156,32 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_chunk_kernel(SampleA
   if (tid == 0) n_list = 0;
   SampleBest b{-INFINITY, INT32_MAX};
 #pragma unroll
-  for (int j = 0; j < V; ++j)
-    if (v[j] > b.v) b = SampleBest{v[j], first + j / 4 * 4 * kSampleThreads + j % 4};
+  for (int j = 0; j < V; ++j) b.v = fmaxf(b.v, v[j]);  // (NaN aside)
+#pragma unroll
+  for (int j = V - 1; j >= 0; --j) b.i = v[j] == b.v ? first + j / 4 * 4 * kSampleThreads + j % 4 : b.i;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) b = best_of(b, SampleBest{__shfl_xor(b.v, o, kWave), __shfl_xor(b.i, o, kWave)});
   if (lane == 0) best[wave] = b;
   __syncthreads();
+  b = best[lane % (kSampleThreads / 64)];
 #pragma unroll
-  for (int w = 0; w < kSampleThreads / 64; ++w) b = best_of(b, best[w]);
+  for (int o = kSampleThreads / 128; o > 0; o >>= 1) b = best_of(b, SampleBest{__shfl_xor(b.v, o, kWave), __shfl_xor(b.i, o, kWave)});
   SampleChunk* out = reinterpret_cast<SampleChunk*>(a.ws) + blockIdx.x;
   if (tid == 0) out->max = b.v, out->index = b.i;
   if (!(t > 0.f) || !(b.v > -INFINITY)) return;  // (greedy, or nothing to choose: the rest is not read)
   const SampleGrid grid = sample_grid(b.v, t);
+  if (b.v == INFINITY) {
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    uint64_t mass;
-    const int at = sample_bin(grid, v[j], &mass);
-    if (at >= 0) lds_add(&bin[at], mass + (1ull << kMassBits));
-    if (j % 2) __builtin_amdgcn_sched_barrier(0);  // (two at a time: all at once take more than 64 registers)
+    for (int j = 0; j < V; ++j)
+      if (v[j] == INFINITY) lds_add(&bin[0], (1ull << 34) + (1ull << kMassBits));
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      uint64_t mass;
+      const double below = bins_below(grid, v[j], &mass);
+      if (below < static_cast<double>(kSampleBins)) lds_add(&bin[whole_bits(below)], mass + (1ull << kMassBits));
+      if (j % 2) __builtin_amdgcn_sched_barrier(0);  // (two at a time: all at once take more than 64 registers)
+    }
   }
   __syncthreads();
   const uint64_t mine = bin[tid];
@@ -162,15 +196,16 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_chunk_kernel(SampleA
   __syncthreads();
   for (int w = 0; w < wave; ++w) n += sums[w];
   const int covered = __syncthreads_count(n <= kSampleList);
-  const double from = grid.top - covered + 1.0;  // (least t of the bins that are covered)
-#pragma unroll
-  for (int j = 0; j < V; ++j) asm volatile("" : "+v"(v[j]));  // (t is formed again, not held from above: 32 registers)
+  // (a range that may hold a few of the next bin's too: with more than there is room for, nothing counts as covered)
+  const float from = covered > 0 ? range_of(grid, 0, covered - 1).lo : INFINITY;
 #pragma unroll
   for (int j = 0; j < V; ++j)
-    if (covered > 0 && (static_cast<double>(v[j]) * grid.per >= from || v[j] == b.v))
-      out->list[atomicAdd(&n_list, 1)] = make_float2(v[j], __int_as_float(first + j / 4 * 4 * kSampleThreads + j % 4));
+    if (v[j] >= from) {
+      const int at = atomicAdd(&n_list, 1);
+      if (at < kSampleList) out->list[at] = make_float2(v[j], __int_as_float(first + j / 4 * 4 * kSampleThreads + j % 4));
+    }
   __syncthreads();
-  if (tid == 0) out->covered = covered, out->listed = n_list;
+  if (tid == 0) out->covered = n_list <= kSampleList ? covered : 0, out->listed = min(n_list, kSampleList);
 }
 
 constexpr int kSampleGather = 4096;  // tokens that the second launch holds in LDS
@@ -214,10 +249,6 @@ __device__ __forceinline__ double weight_up_to(double before, uint64_t mass, dou
   return fma(static_cast<double>(mass), scale, before);
 }
 
-struct SampleRange {
-  float lo, hi;
-  __device__ __forceinline__ bool has(float v) const { return v >= lo && v <= hi; }
-};
 constexpr SampleRange kNoRange{INFINITY, -INFINITY};
 
 // f(logit, index) of a row's logits within either range.  The few that are, of 32 at a time, are marked first and then taken
@@ -251,13 +282,6 @@ __device__ __forceinline__ void each_of_row(const float* x, int vocab, SampleRan
       f(x[i], i);
     }
   }
-}
-
-// A range that holds the logits of bins first .. last, from their edges in t with room for their rounding.
-__device__ __forceinline__ SampleRange range_of(const SampleGrid& grid, int first, int last) {
-  const double lo = (grid.top - last) / grid.per, hi = (grid.top - first + 1.0) / grid.per;
-  return SampleRange{isfinite(lo) ? static_cast<float>(lo - fabs(lo) * 1e-6 - 1e-37) : -INFINITY,
-                     isfinite(hi) ? static_cast<float>(hi + fabs(hi) * 1e-6 + 1e-37) : INFINITY};
 }
 
 __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, int chunks) {
@@ -363,7 +387,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
   if (min_p > 0.f) {
     const double depth = grid.top == static_cast<double>(INFINITY)
                              ? 0.0
-                             : grid.top - floor(static_cast<double>(b.v) * grid.per + 32.0 * log(least));
+                             : grid.top - nearest_whole(static_cast<double>(b.v) * grid.per + 32.0 * log(least));
     if (depth <= static_cast<double>(last_bin)) {
       min_bin = top_bin = low_bin = static_cast<int>(depth);
       want_bins(min_bin, min_bin);
