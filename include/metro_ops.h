@@ -169,7 +169,7 @@ metro_status metro_op_attn_decode_noalloc(const uint16_t* q, const uint16_t* kv,
  * experts: metro_op_rmsnorm_fp8 (with h_bf16), metro_op_gemm with the router's
  * weights, metro_op_route, metro_op_gemm_fp8_experts with gate and up and src,
  * the same with down, and metro_op_combine_experts.  Rows of a QKV product come
- * out plain: RoPE and the write of KV pages are steps of the model alone.
+ * out plain; metro_op_rope_append turns them and writes the KV pages.
  *
  * All are asynchronous on `stream`, allocate nothing and may be captured into a
  * graph; a workspace belongs to one call at a time.  Calls of no rows (no tokens,
@@ -348,8 +348,8 @@ metro_status metro_op_combine_experts(const uint16_t* y, int32_t ldy, int32_t y_
  *   pos, slot device int32 [T]
  *   q         device bf16 [T, nq, hd], 16-byte aligned
  *   kv        device bf16, n_pages pages in the layout above, 16-byte aligned
- * hd 64 or 128, nq <= 1024, nkv <= 256, T * (nq + 2 nkv) <= 2^25, n_pages < 2^27.
- * Errors: E_INVAL. */
+ * Outputs overlap no input.  hd 64 or 128, nq <= 1024, nkv <= 256, T * (nq + 2 nkv)
+ * <= 2^25, n_pages < 2^27.  Errors: E_INVAL. */
 metro_status metro_op_rope_append(const float* qkv_f32, const uint16_t* qkv_bf16, int32_t ld, int32_t T, int32_t nq,
                                   int32_t nkv, int32_t hd, const uint16_t* q_gain, const uint16_t* k_gain, float eps,
                                   const float* rope, int32_t n_pos, const int32_t* pos, const int32_t* slot, uint16_t* q,
@@ -386,8 +386,8 @@ metro_status metro_op_kv_move(uint16_t* kv, int64_t layer_stride, int32_t n_laye
  *   cu_q      device int32 [n_items + 1], ascending, within 0 .. rows
  *   ctx       device int32 [n_items], >= 0
  *   max_q     most queries of an item, 1 .. 4096; later ones are left as they were
- *   max_keys  most keys of an item (ctx + its queries); keys from there on are not
- *             seen.  The larger it is beside the items' own, the fewer workgroups
+ *   max_keys  most keys of an item (ctx + its queries), 1 .. 2^30; keys from there
+ *             on are not seen.  The larger it is beside the items' own, the fewer workgroups
  *             share the keys there are
  *   mask      device uint32 [rows, ldm] or NULL, 32 * ldm >= max_q
  *   block_tables  device int32 [n_items, ldb] page ids, 16 * ldb >= max_keys

@@ -51,7 +51,8 @@ struct TreeArgs {
   float scale;            // 1 / sqrt(hd)
   int items, rows, nq, nkv, hd, n_pages, max_q, max_keys, ldm, ldb;
 };
-constexpr int kTreeMaxQ = 4096;  // queries of an item
+constexpr int kTreeMaxQ = 4096;       // queries of an item
+constexpr int kTreeMaxKeys = 1 << 30;  // keys of an item
 // How a call is cut: `tiles` tiles of `wide` columns (query, head of a group) for each item and kv head, and the keys
 // into `splits` parts of `pairs` page pairs.
 struct TreePlan {

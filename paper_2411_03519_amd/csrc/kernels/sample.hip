@@ -374,13 +374,13 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
 
   // Which bins the searches may end in: each takes the sums at the edges of the bin, or bins, of the one before.
   double lo = sh.with[last_bin], hi = lo;
-  uint32_t tokens_lo = sh.above[last_bin] + sh.count[last_bin], tokens_hi = tokens_lo;
+  uint32_t most = sh.above[last_bin] + sh.count[last_bin];  // tokens
   int top_bin = kSampleBins, low_bin = -1;  // the first and the last of those of the filters
   SampleRange token_range;                  // of the token's
   auto want_bins = [&](int first, int last) {
     for (int k = first + tid; k <= last; k += kSampleThreads) sh.wanted[k] = 1;
     lo = sh.before[first], hi = sh.with[last];
-    tokens_lo = sh.above[first], tokens_hi = sh.above[last] + sh.count[last];
+    most = sh.above[last] + sh.count[last];
   };
   const double least = fmin(static_cast<double>(min_p), 1.0);
   int min_bin = -1;  // the bin that the least weight falls into
@@ -393,14 +393,10 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
       want_bins(min_bin, min_bin);
     }
   }
-  if (top_k > 0 && static_cast<uint32_t>(top_k) < tokens_hi) {
+  if (top_k > 0 && static_cast<uint32_t>(top_k) < most) {
     const int k = search_bins(kByCount, top_k, 0.0);
-    const uint32_t all = tokens_lo;
-    const double before = lo;
     want_bins(k, k);
     top_bin = min(top_bin, k), low_bin = max(low_bin, k);
-    // (in the bin of min_p, which of the two comes first is open)
-    if (k == min_bin && all < static_cast<uint32_t>(top_k)) lo = before, tokens_lo = all;
   }
   const double share = static_cast<double>(fmaxf(top_p, 0.f));
   if (top_p < 1.f) {

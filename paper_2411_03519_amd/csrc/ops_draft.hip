@@ -41,7 +41,8 @@ metro_status check_tree(const char* who, int32_t nq, int32_t nkv, int32_t items,
   if (items < 0 || rows < 0) return report(METRO_E_INVAL, "%s: items or rows < 0", who);
   if (max_q <= 0 || max_q > metro::kTreeMaxQ)
     return report(METRO_E_INVAL, "%s: max_q must be 1 .. %d", who, metro::kTreeMaxQ);
-  if (max_keys <= 0) return report(METRO_E_INVAL, "%s: max_keys must be positive", who);
+  if (max_keys <= 0 || max_keys > metro::kTreeMaxKeys)
+    return report(METRO_E_INVAL, "%s: max_keys must be 1 .. %d", who, metro::kTreeMaxKeys);
   if (static_cast<int64_t>(items) * nkv * ((max_q * g + 15) / 16) > kMaxBlocks || static_cast<int64_t>(items) * max_q > kMaxBlocks)
     return report(METRO_E_INVAL, "%s: more than 2^22 items by queries or by tiles of 16 columns", who);
   return METRO_OK;

@@ -69,7 +69,7 @@ def test_attn_tree_refusals(metro):
     refused(metro, "metro_op_attn_tree", TREE, CACHE + nulls("q", "kv", "cu_q", "ctx", "block_tables", "out") +
             off(8, "q", "out", "workspace") + off(2, "cu_q", "ctx", "mask", "block_tables") +
             [{"nq": 6}, {"nq": 12}, {"nq": 64}, {"nq": 0}, {"n_items": -1}, {"rows": -1}, {"max_q": 0}, {"max_q": 4097, "ldm": 200},
-             {"max_q": 65}, {"ldm": 1}, {"max_keys": 0}, {"max_keys": 65}, {"ldb": 3}, {"workspace_bytes": -1},
+             {"max_q": 65}, {"ldm": 1}, {"max_keys": 0}, {"max_keys": 65}, {"max_keys": (1 << 30) + 1, "ldb": 1 << 27}, {"ldb": 3}, {"workspace_bytes": -1},
              {"n_items": 1 << 21}], b"attn_tree")
 
 

@@ -268,10 +268,14 @@ def test_long_contexts_split(metro, n):
         tree_case(metro, rng, 4, 2, 128, [3500, 5, 1700], [n] * 3, ws=ws)
 
 
-def test_many_items(metro):
+@pytest.mark.parametrize("hd", [64, 128])
+def test_many_items(metro, hd):
+    """Queries enough that the states are merged a query a workgroup, of one split and of two."""
     rng = np.random.default_rng(5)
     ns = [int(x) for x in rng.integers(1, 12, 60)]
-    tree_case(metro, rng, 4, 8, 128, [int(x) for x in rng.integers(0, 300, 60)], ns)
+    ctxs = [int(x) for x in rng.integers(0, 300, 60)]
+    assert metro.op_attn_tree_workspace(32, 8, hd, 60, sum(ns), max(ns), max(c + n for c, n in zip(ctxs, ns))) > 0
+    tree_case(metro, rng, 4, 8, hd, ctxs, ns)
 
 
 def test_peaked_and_rising_scores(metro):
@@ -524,6 +528,17 @@ def test_sample_crowded_logits(metro):
     for kw in (dict(), dict(top_k=[300, 1500, 5000, 1999, 700, 9999]), dict(top_p=[0.5, 0.31, 0.77, 0.9, 0.2, 0.6]),
                dict(temperature=[1e-3, 1e-3, 1e-30, 1.0, 100.0, 1e-42], top_p=[0.8] * 6)):
         sample_case(metro, x, rng.random(6), **kw)
+
+
+@pytest.mark.parametrize("spread", [0.01, 1.0, 20.0])
+def test_sample_many_rows_of_many_settings(metro, spread):
+    rng = np.random.default_rng(int(100 * spread))
+    rows, vocab = 1500, 777
+    x = (spread * rng.standard_normal((rows, vocab))).astype(np.float32)
+    x[::3] = np.round(x[::3] * 4 / spread) * (spread / 4)  # (ties)
+    pick = lambda *v: rng.choice(v, rows)
+    sample_case(metro, x, rng.random(rows), temperature=pick(0.0, 0.2, 0.7, 1.0, 3.0), top_k=pick(0, 1, 5, 30, 300, 776),
+                top_p=pick(0.05, 0.5, 0.9, 0.999, 1.0), min_p=pick(0.0, 0.0, 0.01, 0.3, 0.9))
 
 
 def test_sample_infinities_and_nan(metro):
