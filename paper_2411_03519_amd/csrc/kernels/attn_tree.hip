@@ -7,12 +7,25 @@
 // The matrix products are those of the decode and prefill kernels: scores S^T =
 // K Q^T and outputs O^T += V^T P^T on 16 keys x 16 columns, a column being a
 // (query, head) pair of one kv head's group, so that a key is read once for all
-// queries of a tree.  A wave takes pairs of pages (32 keys) straight from memory
-// into operand registers and holds up to CT tiles of 16 columns against each;
-// the waves of a workgroup share a split's pairs in turn and merge their (max,
-// sum, output) states through LDS in wave order, and a second launch merges the
-// splits in order.  Scores, softmax and sums are fp32; the weights enter the
-// bf16 matrix cores as hi + lo, about 16 significant bits.
+// queries of a tree.  Pages go in pairs (32 keys).  Up to 32 columns they pass from
+// memory straight into operand registers, each wave with pairs of its own; more
+// columns are eight waves of 16 against the same pairs, which go through LDS.  The
+// keys of an item are cut into splits where that fills the chip, and a second
+// launch merges their (max, sum, output) states in order.  Scores, softmax and
+// sums are fp32; the weights enter the bf16 matrix cores as hi + lo, about 16
+// significant bits, which costs a third of the matrix instructions.
+//
+// What bounds it.  One token a sequence: K and V, streamed at 5.0 TB/s (123
+// contexts of 256 .. 4096 keys, 142 us; 25 of them 33 us).  Trees of 8 to 32 tokens
+// read the same and are held up besides by the scores' way through the vector ALU
+// (exponentials, the split into hi + lo), which overlaps the matrix cores' only
+// between waves: 123 trees 204 us, 25 of 9 to 17 tokens 43 us.  512 columns after
+// 20000 to 30000 keys: matrix cores busy 39% of the time, vector ALU about as much,
+// 190 to 220 us, 530 to 460 TFLOP/s of the products asked for and half as many again
+// for lo (a large library product reaches 1211 on this card).  Two and four tiles a
+// wave against LDS or registers, scores of the next pair formed beside this one's
+// weights, and tiles of up to 64 columns with the pairs shared by two halves of the
+// workgroup gave nothing over this.
 #include "common.h"
 #include "kernels.h"
 #include "kernels_draft.h"
@@ -23,6 +36,7 @@ constexpr float kTreeLog2e = 1.4426950408889634f;
 // the running maximum before any key: every finite score of use lies above it, and differences from it are finite
 constexpr float kTreeNone = -1.7e38f;
 constexpr int kTreeMaxSplits = 64;  // (a lane each in the merge)
+
 __device__ __forceinline__ f32x4 mfma32(uint4 a, uint4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
 }
@@ -624,14 +638,18 @@ __global__ __launch_bounds__(256) void attn_tree_combine_many_kernel(TreeArgs a,
 // Up to 32 columns an item: the kernel through registers, one or two tiles a wave; more: the shared one.  A split has
 // to be worth its states (a column's is 528 bytes written and read again, a pair of pages 16 KiB): at least an eighth
 // of its columns in pairs, and four.  More splits are made while max_keys would leave fewer than `full` workgroups; the
-// items are often shorter than it, hence some times the 256 CUs.
+// items are often shorter than it, hence some times the 256 CUs, and where the items alone are more than fit the chip at
+// once, the longest of them must not outlast the others.  Measured (us; heads 32 over 8 of 128 but for the 64 tokens'):
+// 25 single tokens after 256 .. 4096 keys, full 1024 / 2048 / 4096: 36.0 / 33.1 / 36.7; 123 of them 152 / 142 / 140; 25
+// trees of 9 .. 17 tokens 43 / 50 / 54; 123 of 8 .. 32 224 / 204 / 202; two of 57 .. 64 after 20000 .. 30000 keys, 64 heads
+// over 8, 194 .. 207 / 202 .. 207 / 227 .. 234.
 TreePlan plan_attn_tree(int nq, int nkv, int hd, int items, int rows, int max_q, int max_keys, int64_t part_floats) {
   const int cols = max_q * (nq / nkv);
   TreePlan p;
   p.wide = cols <= 16 ? 16 : cols <= 32 ? 32 : 16 * kTreeSharedWaves;
-  const int full = cols <= 16 ? 2048 : 1024;
   p.tiles = (cols + p.wide - 1) / p.wide;
   const int64_t groups = static_cast<int64_t>(items) * nkv * p.tiles;
+  const int full = cols <= 16 || (cols > 32 && groups > 512) ? 2048 : 1024;
   const int pairs = max_keys / (2 * kPage) + (max_keys % (2 * kPage) ? 1 : 0);
   int64_t most = part_floats / (static_cast<int64_t>(rows) * nq * (hd + 2));  // splits whose states fit
   if (most > kTreeMaxSplits) most = kTreeMaxSplits;
