@@ -269,6 +269,32 @@ def test_long_contexts_split(metro, n):
 
 
 @pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n", [1, 8, 20])
+def test_long_contexts_without_splits(metro, hd, n):
+    """More page pairs a wave than a wave holds page ids of at once (64), on both sides of a multiple of it."""
+    rng = np.random.default_rng([hd, n])
+    for ctx in (8192 - n, 8192 + 33, 9000):
+        tree_case(metro, rng, 4, 1, hd, [ctx], [n], ws=0)
+
+
+def test_long_chunks_and_wide_trees(metro):
+    """Chunks of hundreds of queries in many tiles of columns, masks of many words."""
+    rng = np.random.default_rng(21)
+    tree_case(metro, rng, 4, 2, 128, [100, 0, 31], [300, 129, 1], chain=True)
+    tree_case(metro, rng, 8, 1, 64, [70], [210], chain=True, ws=0)
+    tree_case(metro, rng, 2, 2, 128, [45, 200], [200, 31])
+
+
+def test_bounds_larger_than_any_item(metro):
+    """max_q and max_keys of a batch that was planned for more, as a captured one is."""
+    rng = np.random.default_rng(22)
+    for ws in (True, 0):
+        tree_case(metro, rng, 4, 2, 128, [100, 7, 300], [3, 1, 5], max_q=64, max_keys=4096, ws=ws)
+        tree_case(metro, rng, 4, 2, 128, [100, 7], [1, 1], chain=True, max_q=3, max_keys=2000, ws=ws)
+        tree_case(metro, rng, 1, 3, 64, [100, 7], [9, 2], max_q=30, max_keys=500, ws=ws)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
 def test_many_items(metro, hd):
     """Queries enough that the states are merged a query a workgroup, of one split and of two."""
     rng = np.random.default_rng(5)
