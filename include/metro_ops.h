@@ -379,8 +379,9 @@ metro_status metro_op_kv_move(uint16_t* kv, int64_t layer_stride, int32_t n_laye
  * j <= r, a chain); over the keys t that it sees, as metro_op_attn_decode,
  *   out[row, head, :] = bf16( sum_t softmax_t(q . K[t] / sqrt(hd)) V[t] ),
  * zeros where it sees none, or none whose score is above -inf.  What the keys that
- * a query does not see hold (NaN, Inf) does not reach it.  Rows in no item are left
- * as they were.
+ * a query does not see hold (NaN, Inf) does not reach it; an infinity among the
+ * values of the ctx keys makes its outputs infinite or NaN.  Rows in no item are
+ * left as they were.
  *   q         device bf16 [rows, nq, hd], 16-byte aligned
  *   kv        device bf16, n_pages pages in the layout above, 16-byte aligned
  *   cu_q      device int32 [n_items + 1], ascending, within 0 .. rows

@@ -195,10 +195,10 @@ hipError_t launch_rope_append(const AppendArgs& a, hipStream_t s) {
 
 // ---------------------------------------------------------------------------
 // Move.  A thread owns one 16-byte chunk of the K tile (8 dims of a key) or one
-// of the V^T tile (a key's two values there) for all moves of a group: it reads
-// the chunk at every source before it writes the first destination, and writes
-// in the list's order, so no other thread can come between and no barrier is
-// needed.  Grid: (chunks of a layer's heads, layers, groups).  Bound by the lines
+// of the V^T tile (a key's two values there) for all moves of a group: eight moves
+// at a time, it reads the chunk at every source before it writes the first
+// destination, and writes in the list's order, so no other thread can come between
+// and no barrier is needed.  Grid: (chunks of a layer's heads, layers, groups).  Bound by the lines
 // that it touches: a key's 256 bytes of K lie in 16 of them, those of V as 2-byte
 // values in the 1 KiB that its four keys share, so 107 moves in 32 layers of 8 heads
 // read and write about 6 times their 28 MB (22 us; one sequence's 3 moves 3.8).

@@ -338,6 +338,30 @@ def test_masked_values_that_are_not_finite_reach_only_their_queries(metro):
         assert np.isfinite(got[0]).all() and np.isinf(got[2, :, 3]).all()
 
 
+def test_infinite_context_values_stay_in_their_outputs(metro):
+    """An infinity among the context's values: its dim of its head is infinite or NaN, everything else as without it."""
+    rng = np.random.default_rng(25)
+    nq, nkv = 16, 2
+    for hd, n in ((64, 1), (128, 6), (128, 30)):  # (one tile of columns, three, more)
+        K, V = [[bits(rng.standard_normal((200 + n, nkv, hd)))] for _ in range(2)]
+        q = bits(rng.standard_normal((n, nq, hd)))
+
+        def go(values):
+            pool, tables = tree_pool(np.random.default_rng(26), K, [values], nkv, hd)
+            out = empty_bits(n * nq * hd)
+            metro.op_attn_tree(dev(q), dev(pool), len(pool), nq, nkv, hd, 1, ints([0, n]), n, ints([200]), n, 200 + n, ints(tables),
+                               tables.shape[1], out)
+            return bf16_bits_to_f64(host(out)).reshape(n, nkv, nq // nkv, hd)
+
+        plain = go(V[0])
+        odd = V[0].copy()
+        odd[70, 1, 9] = 0x7F80
+        got = go(odd)
+        assert np.isfinite(plain).all() and not np.isfinite(got[:, 1, :, 9]).any()
+        got[:, 1, :, 9] = plain[:, 1, :, 9]
+        assert (got == plain).all()
+
+
 def test_infinite_scores(metro):
     """Scores of -inf weigh nothing, a query with no others gets zeros."""
     rng = np.random.default_rng(10)
