@@ -70,6 +70,7 @@ __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(
 // 2^50 on, where other logits than the largest lie further than all bins below it, bins have no width.
 struct SampleGrid {
   double per, top, step;
+  double width;  // of a bin in logits, 1 / per
 };
 
 // The nearest whole number of |t| < 2^51, ties to even; the adding leaves no room behind the point.
@@ -78,6 +79,7 @@ __device__ __forceinline__ double nearest_whole(double t) { return (t + 67553994
 __device__ __forceinline__ SampleGrid sample_grid(float max, float t) {
   SampleGrid g;
   g.per = 32.0 / static_cast<double>(t);
+  g.width = static_cast<double>(t) / 32.0;
   g.top = max == INFINITY ? static_cast<double>(INFINITY) : nearest_whole(static_cast<double>(max) * g.per);
   g.step = fabs(g.top) < 1125899906842624.0 ? 1.0 / 32.0 : 0.0;
   return g;
@@ -119,7 +121,7 @@ struct SampleRange {
 
 // A range that holds the logits of bins first .. last, from their edges in t with room for their rounding.
 __device__ __forceinline__ SampleRange range_of(const SampleGrid& grid, double first, double last) {
-  const double lo = (grid.top - last - 0.5) / grid.per, hi = (grid.top - first + 0.5) / grid.per;
+  const double lo = (grid.top - last - 0.5) * grid.width, hi = (grid.top - first + 0.5) * grid.width;
   return SampleRange{isfinite(lo) ? static_cast<float>(lo - fabs(lo) * 1e-6 - 1e-37) : -INFINITY,
                      isfinite(hi) ? static_cast<float>(hi + fabs(hi) * 1e-6 + 1e-37) : INFINITY};
 }
@@ -217,11 +219,19 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_chunk_kernel(SampleA
 
 constexpr int kSampleGather = 4096;  // tokens that the second launch holds in LDS (2048: 25 rows 54 us for 48)
 constexpr int kSampleRank = 96;      // tokens that are ranked by comparing all pairs
+constexpr int kSampleRankStep = 4;   // so many at a time (one: 325 rows 106 us for 100; eight: 103)
+static_assert(kSampleRank % kSampleRankStep == 0, "");
 
 constexpr int kSampleSearches = 8;   // for bins, each with room of its own
 
+// A token among those of its bin: `place` is larger for one that stands before it in the row's order, 0 is none.
+struct __attribute__((aligned(16))) SampleToken {
+  uint64_t place, mass;
+};
+
 struct SampleShared {
   double before[kSampleBins], with[kSampleBins];    // weight of the bins above, and with this one
+  double scale[kSampleBins];                        // of a bin's masses
   uint32_t count[kSampleBins], above[kSampleBins];  // tokens of a bin, and of the bins above
   uint64_t sub_mass[kSampleBins];
   uint32_t sub_count[kSampleBins];
@@ -229,14 +239,12 @@ struct SampleShared {
   int index[kSampleGather];
   uint16_t bin[kSampleGather];
   uint8_t wanted[kSampleBins];  // bins that are gathered
-  uint32_t rank_key[kSampleRank];
-  int rank_index[kSampleRank];
-  uint64_t rank_mass[kSampleRank];
+  SampleToken rank[kSampleRank];
   double scan_w[16];
   uint64_t scan_m[16];
   uint32_t scan_c[16];
   int scan_last[16];
-  uint32_t n, some_n;
+  uint32_t n, n_wanted, some_n;
   uint64_t some;
   int first, sub;
   int found_bin[kSampleSearches][kSampleThreads / 64];
@@ -245,6 +253,7 @@ struct SampleShared {
   int found;
   int shift[kSampleChunks];    // bins between the row's largest and a chunk's; all of them where it counts for nothing
   int covered[kSampleChunks];  // bins of a chunk whose tokens are listed
+  int listed[kSampleChunks];   // its list's length
 };
 
 enum SampleWant { kByCount, kReach, kPass };  // the first token whose count, or weight, up to it reaches, or passes, the wanted
@@ -299,9 +308,12 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
   const SampleChunk& own_chunk = chunk[min(lane % kSampleChunks, chunks - 1)];
   SampleBest b{own_chunk.max, own_chunk.index};
   const float chunk_max = b.v;
+  const int own_covered = own_chunk.covered, own_listed = own_chunk.listed;
+  const float t = a.temperature ? a.temperature[row] : 1.f;
+  const float min_p = a.min_p ? a.min_p[row] : 0.f, top_p = a.top_p ? a.top_p[row] : 1.f, u = a.u[row];
+  const int top_k = a.top_k ? a.top_k[row] : 0;
 #pragma unroll
   for (int o = kSampleChunks / 2; o > 0; o >>= 1) b = best_of(b, SampleBest{__shfl_xor(b.v, o, kWave), __shfl_xor(b.i, o, kWave)});
-  const float t = a.temperature ? a.temperature[row] : 1.f;
   if (!(b.v > -INFINITY) || !(t > 0.f)) {
     if (tid == 0) {
       a.out[row] = b.v > -INFINITY ? b.i : -1;
@@ -309,17 +321,16 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
     }
     return;
   }
-  const float min_p = a.min_p ? a.min_p[row] : 0.f, top_p = a.top_p ? a.top_p[row] : 1.f, u = a.u[row];
-  const int top_k = a.top_k ? a.top_k[row] : 0;
   const SampleGrid grid = sample_grid(b.v, t);
   if (tid < chunks) {
     // (an infinite difference, or that of infinities: all of the chunk or nothing)
     const double d = chunk_max == b.v ? 0.0 : grid.top - sample_grid(chunk_max, t).top;
     const bool any = chunk_max > -INFINITY && d < static_cast<double>(kSampleBins);
     sh.shift[tid] = any ? static_cast<int>(d) : kSampleBins;
-    sh.covered[tid] = any ? own_chunk.covered : 0;
+    sh.covered[tid] = any ? own_covered : 0;
+    sh.listed[tid] = any ? own_listed : 0;
   }
-  if (tid == 0) sh.n = 0, sh.some = 0, sh.some_n = 0;
+  if (tid == 0) sh.n = 0, sh.n_wanted = 0, sh.some = 0, sh.some_n = 0;
   sh.wanted[tid] = 0;
   __syncthreads();
 
@@ -359,6 +370,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
   }
   const double my_with = weight_up_to(head + bw, mass, scale_here);
   const uint32_t my_tokens = bc + count;
+  sh.scale[tid] = scale_here;
   sh.before[tid] = head + bw;
   sh.with[tid] = my_with;
   sh.above[tid] = bc;
@@ -368,15 +380,21 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
   // The first bin that holds any token and whose count or weight, with the bins above, is as wanted; the last one with a
   // token where none is.
   int searches = 0;
-  auto search_bins = [&](SampleWant how, uint32_t n, double want) {
-    int(&found)[kSampleThreads / 64] = sh.found_bin[searches++];
+  auto begin_search = [&](SampleWant how, uint32_t n, double want) {
     const uint64_t ok = __ballot(count > 0 && (how == kByCount ? my_tokens >= n : how == kReach ? my_with >= want : my_with > want));
-    if (lane == 0) found[wave] = ok ? 64 * wave + __ffsll(static_cast<unsigned long long>(ok)) - 1 : last_bin;
-    __syncthreads();
+    if (lane == 0) sh.found_bin[searches][wave] = ok ? 64 * wave + __ffsll(static_cast<unsigned long long>(ok)) - 1 : last_bin;
+    return searches++;
+  };
+  auto end_search = [&](int search) {  // (behind a barrier)
     int bin = last_bin;
 #pragma unroll
-    for (int k = 0; k < kSampleThreads / 64; ++k) bin = min(bin, found[k]);
+    for (int k = 0; k < kSampleThreads / 64; ++k) bin = min(bin, sh.found_bin[search][k]);
     return bin;
+  };
+  auto search_bins = [&](SampleWant how, uint32_t n, double want) {
+    const int search = begin_search(how, n, want);
+    __syncthreads();
+    return end_search(search);
   };
 
   // Which bins the searches may end in: each takes the sums at the edges of the bin, or bins, of the one before.
@@ -384,6 +402,14 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
   uint32_t most = sh.above[last_bin] + sh.count[last_bin];  // tokens
   int top_bin = kSampleBins, low_bin = -1;  // the first and the last of those of the filters
   SampleRange token_range;                  // of the token's
+  struct Ends {
+    int first, last;
+  };
+  auto search_ends = [&](SampleWant how, double want_lo, double want_hi) {
+    const int f = begin_search(how, 0, want_lo), l = begin_search(how, 0, want_hi);
+    __syncthreads();
+    return Ends{end_search(f), end_search(l)};
+  };
   auto want_bins = [&](int first, int last) {
     for (int k = first + tid; k <= last; k += kSampleThreads) sh.wanted[k] = 1;
     lo = sh.before[first], hi = sh.with[last];
@@ -407,17 +433,17 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
   }
   const double share = static_cast<double>(fmaxf(top_p, 0.f));
   if (top_p < 1.f) {
-    const int first = search_bins(kReach, 0, share * lo), last = search_bins(kReach, 0, share * hi);
+    const auto [first, last] = search_ends(kReach, share * lo, share * hi);
     want_bins(first, last);
     top_bin = min(top_bin, first), low_bin = max(low_bin, last);
   }
   const double part = static_cast<double>(u > 0.f ? u : 0.f);
   if (u >= 1.f) {
-    const int first = search_bins(kReach, 0, lo), last = search_bins(kReach, 0, hi);
+    const auto [first, last] = search_ends(kReach, lo, hi);
     want_bins(first, last);
     token_range = range_of(grid, first, last);
   } else {
-    const int first = search_bins(kPass, 0, part * lo), last = search_bins(kPass, 0, part * hi);
+    const auto [first, last] = search_ends(kPass, part * lo, part * hi);
     want_bins(first, last);
     token_range = range_of(grid, first, last);
   }
@@ -427,12 +453,9 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
   const bool mine_wanted = sh.wanted[tid] != 0;
   bool listed = true;
   for (int c = 0; c < chunks; ++c) listed &= !mine_wanted || tid < sh.shift[c] + sh.covered[c];
-  if (mine_wanted && count > 0) atomicAdd(&sh.n, count);
+  if (mine_wanted && count > 0) atomicAdd(&sh.n_wanted, count);
   const bool lists = __syncthreads_and(listed);
-  const bool gather = sh.n <= kSampleGather;
-  __syncthreads();
-  if (tid == 0) sh.n = 0;
-  __syncthreads();
+  const bool gather = sh.n_wanted <= kSampleGather;
   auto take = [&](float v, int i) {
     uint64_t m;
     const int at = sample_bin(grid, v, &m);
@@ -444,9 +467,9 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
     if (lists) {
 #pragma unroll
       for (int k = 0; k < kSampleChunks * kSampleList / kSampleThreads; ++k) {
-        const int at = tid + k * kSampleThreads, c = at / kSampleList;
-        if (c >= chunks || sh.shift[c] >= kSampleBins || at % kSampleList >= chunk[c].listed) continue;
-        const float2 e = chunk[c].list[at % kSampleList];
+        const int c = (tid + k * kSampleThreads) / kSampleList;
+        if (c >= chunks || tid % kSampleList >= sh.listed[c]) continue;
+        const float2 e = chunk[c].list[tid % kSampleList];
         take(e.x, __float_as_int(e.y));
       }
     } else {
@@ -477,7 +500,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
       each_of_row(x, vocab, range_of(grid, min_bin, min_bin), kNoRange, [&](float v, int) { add(v); });
     }
     __syncthreads();
-    total = weight_up_to(sh.before[min_bin], sh.some, bin_scale(min_bin));
+    total = weight_up_to(sh.before[min_bin], sh.some, sh.scale[min_bin]);
     tokens = sh.above[min_bin] + sh.some_n;
   }
 
@@ -490,7 +513,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
     if (step == 1 && !(top_p < 1.f)) continue;
     const uint32_t want_n = top_k;
     const int bin = search_bins(how, want_n, want);
-    const double before = sh.before[bin], scale = bin_scale(bin);
+    const double before = sh.before[bin], scale = sh.scale[bin];
     const uint32_t above = sh.above[bin];
     const bool from_row = !gather || !sh.wanted[bin];
     auto there = [&](uint32_t c, uint64_t m) {
@@ -594,38 +617,41 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
       }
     } else {
       if (tid == 0) sh.n = 0;
+      if (tid < kSampleRank) sh.rank[tid] = SampleToken{0, 0};
       __syncthreads();
       each([&](uint32_t k, int i, uint64_t m) {
         if (k < klo || k > khi) return;
         const uint32_t at = atomicAdd(&sh.n, 1u);
-        if (at < kSampleRank) sh.rank_key[at] = k, sh.rank_index[at] = i, sh.rank_mass[at] = m;
+        if (at < kSampleRank) sh.rank[at] = SampleToken{static_cast<uint64_t>(k) << 32 | ~static_cast<uint32_t>(i), m};
       });
       __syncthreads();
       const int have = min(sh.n, static_cast<uint32_t>(kSampleRank));
       if (tid < have) {
-        const uint32_t key = sh.rank_key[tid];
-        const int at = sh.rank_index[tid];
-        const uint64_t own = sh.rank_mass[tid];
+        const uint64_t place = sh.rank[tid].place, own = sh.rank[tid].mass;
         uint64_t m = base_m;
         uint32_t rank = 0;
-        for (int j = 0; j < have; ++j) {
-          const uint32_t k = sh.rank_key[j];
-          const bool higher = k > key || (k == key && sh.rank_index[j] < at);
-          m += higher ? sh.rank_mass[j] : 0;
-          rank += higher ? 1 : 0;
+        for (int j = 0; j < have; j += kSampleRankStep) {
+          SampleToken other[kSampleRankStep];
+#pragma unroll
+          for (int e = 0; e < kSampleRankStep; ++e) other[e] = sh.rank[j + e];
+#pragma unroll
+          for (int e = 0; e < kSampleRankStep; ++e) {
+            const bool higher = other[e].place > place;
+            m += higher ? other[e].mass : 0;
+            rank += higher ? 1 : 0;
+          }
         }
         // the first that is as wanted, or the last
         const bool ok = there(base_c + rank + 1, m + own);
         if (ok ? rank == 0 || !there(base_c + rank, m) : static_cast<int>(rank) == have - 1) {
           sh.upto = weight_up_to(before, m + own, scale);
           sh.own = static_cast<double>(own) * scale;
-          sh.found = at;
+          sh.found = static_cast<int>(~static_cast<uint32_t>(place));
         }
       }
     }
     __syncthreads();
-    if (step < 2) total = fmin(total, sh.upto);
-    __syncthreads();
+    if (step < 2) total = fmin(total, sh.upto);  // (the next step writes it behind its search's barrier)
   }
   if (tid == 0) {
     a.out[row] = sh.found;
