@@ -421,12 +421,13 @@ metro_status metro_op_attn_tree_workspace(int32_t nq, int32_t nkv, int32_t hd, i
  *          u[r] times the sum of the kept ones
  *   prob[r] = its w / that sum, unless prob is NULL
  * so u = 0 gives the most likely token, and u uniform on [0, 1) samples.  u below 0
- * or NaN counts as 0, from 1 on it gives the last kept token.  Weights are
- * held to 2^-35 of themselves, those below 2^-46 may count as none (of 2^18 they
- * change the sums by less than 2^-28).  temperature 0,
- * below 0 or NaN is the greedy choice (metro_op_argmax, prob 1).  A NaN setting
- * otherwise counts as not set; a NULL array sets none (temperature 1).  NaN logits
- * are skipped; out is -1 and prob 0 where none is above -inf.
+ * or NaN counts as 0, from 1 on it gives the last kept token, however little its
+ * weight adds to the sum.  Weights are held to 2^-35 of themselves; tokens whose
+ * weights lie below 2^-46 may count as not there (of 2^18 they change the sums by
+ * less than 2^-28).  temperature 0, below 0 or NaN is the greedy choice
+ * (metro_op_argmax, prob 1).  A NaN setting otherwise counts as not set; a NULL
+ * array sets none (temperature 1).  NaN logits are skipped; out is -1 and prob 0
+ * where none is above -inf.
  *   logits  device fp32 [rows, ldl], ldl >= vocab
  *   temperature, top_p, min_p, u  device fp32 [rows];  top_k, out  device int32 [rows]
  *   prob    device fp32 [rows] or NULL

@@ -103,5 +103,5 @@ def sample(x, u: float, temperature: float = 1.0, top_k: int = 0, top_p: float =
     total = math.fsum(w)
     upto = np.cumsum(w)
     at = int(np.searchsorted(upto, (u if u > 0 else 0.0) * total, side="right"))
-    at = min(at, len(w) - 1)
+    at = len(w) - 1 if u >= 1 else min(at, len(w) - 1)
     return int(tokens[at]), float(w[at] / total)

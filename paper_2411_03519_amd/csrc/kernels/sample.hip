@@ -5,7 +5,10 @@
 // all but the first k, top-p all but the shortest beginning that holds top_p of
 // what is left; the token is the first whose weights up to it pass u times the
 // weights that are left.  All three leave a beginning of the order, so the steps
-// need nothing but searches of the running sums of weights and of counts.
+// need nothing but searches of the running sums of weights and of counts.  From
+// u = 1 on the last token left is found by its count: the sums round, and a weight
+// that they lose, or the same sum formed another way, would end such a search early
+// or late.
 //
 // A search goes by a histogram.  Bins lie about the whole numbers of t = 32 x / T,
 // the same for every part of a row, counted down from the row's largest; 1024 of them
@@ -249,9 +252,11 @@ struct SampleShared {
   uint64_t some;
   int first, sub;
   int found_bin[kSampleSearches][kSampleThreads / 64];
-  // what a search leaves: the weights up to its token and with it, the token's own weight and index
+  // what a search leaves: the weights up to its token and with it, the token's own weight, its index, and how many tokens
+  // of the order it ends
   double upto, own;
   int found;
+  uint32_t ends;
   int shift[kSampleChunks];    // bins between the row's largest and a chunk's; all of them where it counts for nothing
   int covered[kSampleChunks];  // bins of a chunk whose tokens are listed
   int listed[kSampleChunks];   // its list's length
@@ -390,7 +395,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
     int bin = last_bin;
 #pragma unroll
     for (int k = 0; k < kSampleThreads / 64; ++k) bin = min(bin, sh.found_bin[search][k]);
-    return bin;
+    return __builtin_amdgcn_readfirstlane(bin);
   };
   auto search_bins = [&](SampleWant how, uint32_t n, double want) {
     const int search = begin_search(how, n, want);
@@ -400,21 +405,21 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
 
   // Which bins the searches may end in: each takes the sums at the edges of the bin, or bins, of the one before.
   double lo = sh.with[last_bin], hi = lo;
-  uint32_t most = sh.above[last_bin] + sh.count[last_bin];  // tokens
+  uint32_t most = sh.above[last_bin] + sh.count[last_bin], fewest = most;  // tokens
   int top_bin = kSampleBins, low_bin = -1;  // the first and the last of those of the filters
   SampleRange token_range;                  // of the token's
   struct Ends {
     int first, last;
   };
-  auto search_ends = [&](SampleWant how, double want_lo, double want_hi) {
-    const int f = begin_search(how, 0, want_lo), l = begin_search(how, 0, want_hi);
+  auto search_ends = [&](SampleWant how, uint32_t n_lo, uint32_t n_hi, double want_lo, double want_hi) {
+    const int f = begin_search(how, n_lo, want_lo), l = begin_search(how, n_hi, want_hi);
     __syncthreads();
     return Ends{end_search(f), end_search(l)};
   };
   auto want_bins = [&](int first, int last) {
     for (int k = first + tid; k <= last; k += kSampleThreads) sh.wanted[k] = 1;
     lo = sh.before[first], hi = sh.with[last];
-    most = sh.above[last] + sh.count[last];
+    fewest = sh.above[first], most = sh.above[last] + sh.count[last];
   };
   const double least = fmin(static_cast<double>(min_p), 1.0);
   int min_bin = -1;  // the bin that the least weight falls into
@@ -429,22 +434,20 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
   }
   if (top_k > 0 && static_cast<uint32_t>(top_k) < most) {
     const int k = search_bins(kByCount, top_k, 0.0);
+    const uint32_t n = min(fewest, static_cast<uint32_t>(top_k));
     want_bins(k, k);
+    fewest = n, most = top_k;
     top_bin = min(top_bin, k), low_bin = max(low_bin, k);
   }
   const double share = static_cast<double>(fmaxf(top_p, 0.f));
   if (top_p < 1.f) {
-    const auto [first, last] = search_ends(kReach, share * lo, share * hi);
+    const auto [first, last] = search_ends(kReach, 0, 0, share * lo, share * hi);
     want_bins(first, last);
     top_bin = min(top_bin, first), low_bin = max(low_bin, last);
   }
   const double part = static_cast<double>(u > 0.f ? u : 0.f);
-  if (u >= 1.f) {
-    const auto [first, last] = search_ends(kReach, lo, hi);
-    want_bins(first, last);
-    token_range = range_of(grid, first, last);
-  } else {
-    const auto [first, last] = search_ends(kPass, part * lo, part * hi);
+  {
+    const auto [first, last] = search_ends(u >= 1.f ? kByCount : kPass, fewest, most, part * lo, part * hi);
     want_bins(first, last);
     token_range = range_of(grid, first, last);
   }
@@ -508,11 +511,11 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
   // top-k, top-p, the token
 #pragma unroll 1
   for (int step = 0; step < 3; ++step) {
-    SampleWant how = step == 0 ? kByCount : step == 1 || u >= 1.f ? kReach : kPass;
-    const double want = step == 1 ? share * total : u >= 1.f ? total : part * total;
+    const SampleWant how = step == 1 ? kReach : step == 0 || u >= 1.f ? kByCount : kPass;
+    const double want = (step == 1 ? share : part) * total;
     if (step == 0 && !(top_k > 0 && static_cast<uint32_t>(top_k) < tokens)) continue;
     if (step == 1 && !(top_p < 1.f)) continue;
-    const uint32_t want_n = top_k;
+    const uint32_t want_n = step == 0 ? static_cast<uint32_t>(top_k) : tokens;
     const int bin = search_bins(how, want_n, want);
     const double before = sh.before[bin], scale = sh.scale[bin];
     const uint32_t above = sh.above[bin];
@@ -592,6 +595,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
       if (tid == 0) {
         sh.upto = weight_up_to(before, base_m + nth * m1, scale);
         sh.own = static_cast<double>(m1) * scale;
+        sh.ends = above + base_c + nth;
       }
       if (step == 2) {
         const int span = (vocab + kSampleThreads - 1) / kSampleThreads, i0 = tid * span, i1 = min(i0 + span, vocab);
@@ -648,11 +652,13 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a, in
           sh.upto = weight_up_to(before, m + own, scale);
           sh.own = static_cast<double>(own) * scale;
           sh.found = static_cast<int>(~static_cast<uint32_t>(place));
+          sh.ends = above + base_c + rank + 1;
         }
       }
     }
     __syncthreads();
-    if (step < 2) total = fmin(total, sh.upto);  // (the next step writes it behind its search's barrier)
+    // (the next step writes them behind its search's barrier)
+    if (step < 2) total = fmin(total, sh.upto), tokens = min(tokens, sh.ends);
   }
   if (tid == 0) {
     a.out[row] = sh.found;

@@ -68,6 +68,21 @@ def test_filters_keep_beginnings_of_the_order():
     assert D.sample([1.0, math.inf, 3.0, math.inf], 0.9) == (3, 0.5)
 
 
+def test_u_from_one_on_is_the_last_kept_token():
+    """Also where its weight is lost in the running sums."""
+    x = np.zeros(200000)
+    x[777] = -31.0
+    for u in (1.0, 5.0, math.inf):
+        assert D.sample(x, u)[0] == 777
+        assert D.sample(x, u, min_p=0.5)[0] == 199999
+        assert D.sample(x, u, top_k=1000)[0] == 1000  # (777 is the last of all)
+        assert D.sample(np.zeros(7), u, top_p=0.5)[0] == 3
+    rng = np.random.default_rng(3)
+    for _ in range(50):
+        x = rng.standard_normal(1000)
+        assert D.sample(x, 1.0)[0] == int(np.argmin(x))
+
+
 def test_moves_read_before_they_write():
     hd = 64
     pool = np.arange(2 * 2 * 2 * 1 * 16 * hd, dtype=np.uint16).reshape(2, 2, 2, 1, 16 * hd)

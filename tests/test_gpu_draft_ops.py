@@ -543,6 +543,53 @@ def test_sample_bounds_of_u(metro):
         assert tokens[0] == tokens[4] == tokens[5] == tokens[7] == int(np.argmax(x[0])) and tokens[2] == tokens[3] == tokens[6]
 
 
+def clear_border(x, temperature):
+    """Rows without weights between 2^-46.3 and 2^-45.9, which may or may not count as none."""
+    t = np.asarray(temperature, np.float64).reshape(-1, 1)
+    bits_below = (x.max(axis=1, keepdims=True).astype(np.float64) - x) / t / np.log(2.0)
+    x = np.where((bits_below > 45.9) & (bits_below < 46.3), x - (0.5 * t).astype(np.float32), x).astype(np.float32)
+    bits_below = (x.max(axis=1, keepdims=True).astype(np.float64) - x) / t / np.log(2.0)
+    assert not ((bits_below > 45.9) & (bits_below < 46.3)).any()
+    return x
+
+
+@pytest.mark.parametrize("vocab", [777, 5000])
+@pytest.mark.parametrize("temperature", [0.5, 1.0, 1.7])
+def test_sample_last_kept_token(metro, vocab, temperature):
+    """u from 1 on gives the last kept token: rows in many of which the bin of min-p's least weight holds tokens and keeps
+    none, so that the sum that is left and the last token's own are rounded apart."""
+    rng = np.random.default_rng([vocab, int(10 * temperature)])
+    rows = 240
+    x = clear_border((2.0 * rng.standard_normal((rows, vocab))).astype(np.float32), np.full(rows, temperature))
+    u = rng.choice([1.0, 5.0, np.inf], rows)
+    pick = lambda *v: rng.choice(v, rows)
+    t = np.full(rows, temperature)
+    for kw in (dict(), dict(min_p=pick(0.001, 0.02, 0.05, 0.1)), dict(min_p=pick(0.001, 0.05), top_k=pick(3, 40, 300, 10 ** 6)),
+               dict(min_p=pick(0.001, 0.05), top_p=pick(0.3, 0.9, 0.999)), dict(top_k=pick(1, 60, 700), top_p=pick(0.2, 0.95)),
+               dict(min_p=pick(0.0, 0.01), top_k=pick(0, 20, 500), top_p=pick(1.0, 0.99))):
+        sample_case(metro, x, u, temperature=t, **kw)
+
+
+def test_sample_last_kept_token_of_light_tails(metro):
+    """Weights that the running sums lose, alone in their bin, crowded in it, and equal."""
+    rng = np.random.default_rng(41)
+    vocab = 200000
+    one = np.zeros(vocab, np.float32)
+    one[777] = -31.0
+    some = np.zeros(vocab, np.float32)
+    some[rng.permutation(vocab)[:300]] = (-31.0 - 0.01 * rng.random(300)).astype(np.float32)
+    same = np.zeros(vocab, np.float32)
+    same[rng.permutation(vocab)[:5000]] = -30.5
+    none = np.zeros(vocab, np.float32)
+    none[5] = -40.0  # (below 2^-46: as good as not there)
+    x = np.stack([one, some, same, none] * 3)
+    u = np.repeat([1.0, 7.0, np.inf], 4)
+    sample_case(metro, x, u)
+    sample_case(metro, x, u, top_k=[vocab - 1, vocab - 150, vocab - 2500, vocab - 1] * 3)
+    sample_case(metro, x, u, min_p=[0.5, 3.425e-14, 5e-14, 1e-13] * 3)  # (none of one's, some of some's, all of same's)
+    sample_case(metro, x, u, top_p=[0.9] * 12)
+
+
 def test_sample_odd_settings(metro):
     rng = np.random.default_rng(2)
     x = logits(rng, 8, 3001)
