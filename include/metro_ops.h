@@ -358,10 +358,12 @@ metro_status metro_op_rope_append(const float* qkv_f32, const uint16_t* qkv_bf16
 /* Keys and values from slot to slot of the cache, in n_layers layers whose pages
  * lie layer_stride elements apart: for each group g of moves and j = offsets[g] ..
  * offsets[g+1] - 1 in order, dst[j] <- src[j], as if all sources of a group were
- * read before its first destination is written (groups of more than 8 moves: of
- * 8 at a time, in order, which is the same where a group's moves rise and none
- * goes up, dst[j] <= src[j]).  A later move of a group to the same slot wins.  A
- * slot that one group writes is neither read nor written by another.  Moves from
+ * read before its first destination is written.  Groups of more than 8 moves go 8
+ * at a time, in order, which is the same where no move of an earlier 8 writes a
+ * later one's source: so for an accepted path, listed in the order of its tokens and
+ * brought to places at or before theirs in the sequence, in whatever order the
+ * sequence's pages have their ids.  A later move of a group to the same slot wins.
+ * A slot that one group writes is neither read nor written by another.  Moves from
  * or to a slot outside 0 .. 16 n_pages - 1 are left out.
  *   kv        device bf16, 16-byte aligned; layer_stride % 8 == 0, at least n_pages
  *             pages (not looked at for one layer)

@@ -484,6 +484,43 @@ def test_move_of_long_paths_and_wild_offsets(metro):
     np.testing.assert_array_equal(host(kv), D.kv_move(pool, hd, [9, 70, 11], [1, 3, 2], [0, 3]))
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n", [9, 16, 17, 40])
+def test_move_of_paths_over_pages_in_any_order(metro, hd, n):
+    """Accepted paths of more moves than are read at once, to places among their own sources, over pages whose ids fall or
+    have no order: as if all sources were read first."""
+    rng = np.random.default_rng([hd, n])
+    nkv, n_pages = 2, 24
+    for ids in (np.arange(n_pages)[::-1], rng.permutation(n_pages)):
+        for layers, first in ((1, 0), (2, 13)):
+            pool = rng.integers(0, 1 << 16, size=(layers, n_pages, 2, nkv, 16 * hd), dtype=np.uint16)
+            src, dst, off = [], [], [0]
+            for seq in range(3):
+                at = lambda o: ids[8 * seq + o // 16] * 16 + o % 16
+                # the root, then nodes at or behind the path's own places, close to them
+                nodes = first + np.arange(n) + np.concatenate([[0], np.sort(rng.integers(0, 20 + 3 * seq, n - 1))])
+                src += [int(at(o)) for o in nodes]
+                dst += [int(at(first + j)) for j in range(n)]
+                off.append(len(src))
+            kv = dev(pool)
+            metro.op_kv_move(kv, layers, n_pages, nkv, hd, ints(src), ints(dst), ints(off), 3, len(src))
+            np.testing.assert_array_equal(host(kv), D.kv_move(pool, hd, src, dst, off))
+
+
+def test_long_exchanges_go_eight_at_a_time(metro):
+    rng = np.random.default_rng(42)
+    hd, nkv, n_pages = 64, 2, 10
+    pool = rng.integers(0, 1 << 16, size=(1, n_pages, 2, nkv, 16 * hd), dtype=np.uint16)
+    slots = rng.permutation(n_pages * 16)[:30]
+    src, dst = slots, np.roll(slots, -1)
+    want = pool
+    for lo in range(0, 30, 8):
+        want = D.kv_move(want, hd, src[lo:lo + 8], dst[lo:lo + 8], [0, len(src[lo:lo + 8])])
+    kv = dev(pool)
+    metro.op_kv_move(kv, 1, n_pages, nkv, hd, ints(src), ints(dst), ints([0, 30]), 1, 30)
+    np.testing.assert_array_equal(host(kv), want)
+
+
 # --- sample --------------------------------------------------------------------------
 
 
