@@ -463,9 +463,12 @@ def op_combine_experts(y, y_rows: int, weights, slot, T: int, top_k: int, d: int
 
 def op_rope_append(qkv, T: int, nq: int, nkv: int, hd: int, rope, n_pos: int, pos, slot, q, kv, n_pages: int, q_gain=None,
                    k_gain=None, eps: float = 1e-5, ld: int | None = None, stream=None):
-    """Rows of a QKV product (float32 or bfloat16) -> rotated queries q and keys and
-    values in the cache's slots, normalised by head where a gain is given."""
-    half = qkv is not None and qkv.element_size() == 2
+    """Rows of a QKV product (float32, or bfloat16 or its bits) -> rotated queries q and
+    keys and values in the cache's slots, normalised by head where a gain is given."""
+    import torch
+    half = qkv is not None and qkv.dtype is not torch.float32
+    if half and qkv.dtype not in (torch.bfloat16, torch.int16, torch.uint16):
+        raise ValueError(f"qkv must be float32 or bfloat16 (or its bits in 16-bit integers), not {qkv.dtype}")
     check(lib.metro_op_rope_append(None if half else _ptr(qkv), _ptr(qkv) if half else None,
                                    (nq + 2 * nkv) * hd if ld is None else ld, T, nq, nkv, hd, _ptr(q_gain), _ptr(k_gain),
                                    eps, _ptr(rope), n_pos, _ptr(pos), _ptr(slot), _ptr(q), _ptr(kv), n_pages,

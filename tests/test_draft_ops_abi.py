@@ -59,6 +59,16 @@ def test_rope_append_refusals(metro):
              {"nq": 0}, {"nq": 1025}, {"n_pos": 0}], b"rope_append")
 
 
+def test_rope_append_takes_no_other_types(metro):
+    """Rows of another type are not read as bf16 or as fp32."""
+    torch = pytest.importorskip("torch")
+    for dtype in (torch.float16, torch.float64, torch.int32, torch.int8, torch.float8_e4m3fn):
+        with pytest.raises(ValueError, match="float32 or bfloat16"):
+            metro.op_rope_append(torch.zeros(3, 1024, dtype=dtype), 3, 8, 4, 64, None, 64, None, None, None, None, 9, stream=0)
+    # (none at all: the call of no rows)
+    metro.op_rope_append(None, 0, 8, 4, 64, None, 64, None, None, None, None, 9, stream=0)
+
+
 def test_kv_move_refusals(metro):
     refused(metro, "metro_op_kv_move", MOVE, CACHE + nulls("kv", "src", "dst", "offsets") + off(2, "src", "dst", "offsets") +
             [{"n_layers": -1}, {"n_layers": 65536}, {"n_groups": -1}, {"n_groups": 65536}, {"n_moves": -1},
