@@ -335,8 +335,9 @@ metro_status metro_op_combine_experts(const uint16_t* y, int32_t ldy, int32_t y_
  *                                             with k_gain (NULL: no norm)
  *   (y_i, y_{i+hd/2}) <- (y_i c - y_{i+hd/2} s, y_i s + y_{i+hd/2} c),  i < hd/2,
  *                  (c, s) = rope[pos[t], i]   query and key heads
- * in fp32, rounded to bf16 once: queries to q[t], keys and values to the cache's
- * slot[t] (page * 16 + offset).  A row whose slot lies outside 0 .. 16 n_pages - 1
+ * in fp32, the sum of the squares too (a head whose sum passes it comes out as 0),
+ * rounded to bf16 once: queries to q[t], keys and values to the cache's slot[t]
+ * (page * 16 + offset).  A row whose slot lies outside 0 .. 16 n_pages - 1
  * (a padded batch's) leaves the cache as it is, its queries are written all the
  * same.  A position outside 0 .. n_pos - 1 makes the row's queries and keys NaN.
  * Slots of different rows differ; of rows with the same slot the cache keeps
@@ -380,7 +381,8 @@ metro_status metro_op_kv_move(uint16_t* kv, int64_t layer_stride, int32_t n_laye
  * 1 and key ctx[i] + j where bit j % 32 of mask[row, j / 32] is set (mask NULL: for
  * j <= r, a chain); over the keys t that it sees, as metro_op_attn_decode,
  *   out[row, head, :] = bf16( sum_t softmax_t(q . K[t] / sqrt(hd)) V[t] ),
- * zeros where it sees none, or none whose score is above -inf.  What the keys that
+ * zeros where it sees none, or none whose score is above -inf.  Sums are fp32 and
+ * divided at the end: values up to 2^89 in magnitude stay finite.  What the keys that
  * a query does not see hold (NaN, Inf) does not reach it; an infinity among the
  * values of the ctx keys makes its outputs infinite or NaN.  Rows in no item are
  * left as they were.
@@ -424,12 +426,12 @@ metro_status metro_op_attn_tree_workspace(int32_t nq, int32_t nkv, int32_t hd, i
  *   prob[r] = its w / that sum, unless prob is NULL
  * so u = 0 gives the most likely token, and u uniform on [0, 1) samples.  u below 0
  * or NaN counts as 0, from 1 on it gives the last kept token, however little its
- * weight adds to the sum.  Weights are held to 2^-35 of themselves; tokens whose
- * weights lie below 2^-46 may count as not there (of 2^18 they change the sums by
- * less than 2^-28).  temperature 0, below 0 or NaN is the greedy choice
- * (metro_op_argmax, prob 1).  A NaN setting otherwise counts as not set; a NULL
- * array sets none (temperature 1).  NaN logits are skipped; out is -1 and prob 0
- * where none is above -inf.
+ * weight adds to the sum.  Weights are held to 2^-35 of themselves (to 2^-51 |x /
+ * temperature|, where that is more); tokens whose weights lie below 2^-46 may count
+ * as not there (of 2^18 they change the sums by less than 2^-28).  temperature 0,
+ * below 0 or NaN is the greedy choice (metro_op_argmax, prob 1).  A NaN setting
+ * otherwise counts as not set; a NULL array sets none (temperature 1).  NaN logits
+ * are skipped; out is -1 and prob 0 where none is above -inf.
  *   logits  device fp32 [rows, ldl], ldl >= vocab
  *   temperature, top_p, min_p, u  device fp32 [rows];  top_k, out  device int32 [rows]
  *   prob    device fp32 [rows] or NULL

@@ -152,6 +152,26 @@ def test_append_slots_in_any_order(metro, hd):
     append_case(metro, rng, 8, 2, hd, np.arange(32), np.full(32, -1), 2, False, True, True)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("half", [False, True])
+def test_append_norm_of_heads_whose_squares_pass_fp32(metro, hd, half):
+    """Such a head comes out as 0 (|y| up to 1e18 does not: 128 of their squares are below 2^128), its values as they are."""
+    rng = np.random.default_rng([hd, half])
+    nq, nkv, T = 4, 2, 9
+    append_case(metro, rng, nq, nkv, hd, np.arange(T), np.arange(T), 1, half, True, True, size=2e17)
+    y = (rng.standard_normal((T, nq + 2 * nkv, hd))).astype(np.float32)
+    y[:, 1] = y[:, nq] = 1e25
+    yb, gain = bits(y), dev(bits(np.ones(hd)))
+    kv, q = dev(np.zeros(2 * nkv * 16 * hd, np.uint16)), empty_bits(T * nq * hd)
+    metro.op_rope_append(dev(yb).view(torch.bfloat16) if half else dev(y), T, nq, nkv, hd, dev(rope_table(T, hd)), T, ints(np.arange(T)),
+                         ints(np.arange(T)), q, kv, 1, q_gain=gain, k_gain=gain, eps=EPS)
+    q = bf16_bits_to_f64(host(q)).reshape(T, nq, hd)
+    k = bf16_bits_to_f64(host(kv)).reshape(2, nkv, 16 * hd)[0][:, D.tile_places(hd)[0][:T]]
+    assert (q[:, 1] == 0).all() and (k[0] == 0).all()
+    for x in (q[:, 0], q[:, 2], q[:, 3], k[1]):
+        assert np.isfinite(x).all() and (x != 0).any(axis=1).all()
+
+
 def test_append_norm_of_small_and_large_rows(metro):
     rng = np.random.default_rng(8)
     for size in (0.0, 1e-6, 1e6, 1e15):
@@ -311,6 +331,20 @@ def test_peaked_and_rising_scores(metro):
     tree_case(metro, rng, 4, 2, 128, [490], [10], scale=2.0, K=K, slack=2.0 ** -14)
     K = [bits(rng.standard_normal((500, 2, 128)) * (2.7 - np.arange(500) / 200)[:, None, None])]
     tree_case(metro, rng, 4, 2, 128, [490], [10], scale=2.0, K=K, slack=2.0 ** -14)
+
+
+def test_values_up_to_2_to_the_89(metro):
+    """The weights' sums times such values stay within fp32, with scores that rise (a weight may be 2^8 until the maximum that
+    it is relative to moves on)."""
+    rng = np.random.default_rng(27)
+    for hd, G, n, ctx in ((128, 4, 1, 900), (64, 8, 4, 300), (128, 4, 30, 2000)):  # (one tile of columns, two, more)
+        rise = (0.2 + 3.0 * np.arange(ctx + n) / (ctx + n))[:, None, None]
+        K = [bits(rng.standard_normal((ctx + n, 2, hd)) * rise)]
+        V = [bits(np.clip(rng.standard_normal((ctx + n, 2, hd)), -1.99, 1.99) * 2.0 ** 88)]
+        for ws in (True, 0):
+            # (|z| up to 32 * 4, as above)
+            got = tree_case(metro, rng, G, 2, hd, [ctx], [n], scale=2.0, K=K, V=V, ws=ws, slack=2.0 ** -14)
+            assert np.isfinite(got).all()
 
 
 def test_masks_that_leave_rows_empty(metro):
