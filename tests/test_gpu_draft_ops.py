@@ -741,6 +741,116 @@ def test_sample_follows_the_distribution(metro):
     assert np.all(np.abs(counts - n * p) <= 6 * np.sqrt(n * p * (1 - p)))
 
 
+# --- nothing outside the buffers -----------------------------------------------------
+
+GUARD = 1 << 16  # bytes before and behind a buffer
+INT_MIN, INT_MAX = -2 ** 31, 2 ** 31 - 1
+
+
+class Guarded:
+    """A device buffer between guards of a known pattern."""
+
+    def __init__(self, content):
+        raw = np.ascontiguousarray(content).view(np.uint8).ravel()
+        self.n = raw.size
+        self.was = np.random.default_rng(77).integers(0, 256, 2 * GUARD, dtype=np.uint8)
+        self.all = dev(np.concatenate([self.was[:GUARD], raw, self.was[GUARD:]]))
+        self.inner = self.all[GUARD:GUARD + self.n]
+
+    def read(self, dtype):
+        """The buffer's content, once its guards are as they were."""
+        a = host(self.all)
+        np.testing.assert_array_equal(a[:GUARD], self.was[:GUARD])
+        np.testing.assert_array_equal(a[GUARD + self.n:], self.was[GUARD:])
+        return a[GUARD:GUARD + self.n].view(dtype)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_append_touches_nothing_outside(metro, hd):
+    """Slots on both sides of the cache's ends, in runs and alone; positions outside the table."""
+    rng = np.random.default_rng([hd, 50])
+    nq, nkv, n_pages, end = 4, 2, 3, 48
+    slot = np.array([end - 2, end - 1, end, end + 1, end, end + 1, end + 2, end + 3, -4, -3, -2, -1, -1, 0, 1, 2, 3, 20, INT_MIN,
+                     INT_MAX, INT_MAX - 3, INT_MAX - 2, INT_MAX - 1, end + 16, 44], np.int64)
+    pos = rng.integers(0, 30, len(slot))
+    pos[[1, 4, 17]] = INT_MIN, INT_MAX, -1
+    T, width = len(slot), (nq + 2 * nkv) * hd
+    y = rng.standard_normal((T, width)).astype(np.float32)
+    rope = rope_table(30, hd)
+    pool = rng.choice(NAN_BITS, size=(n_pages, 2, nkv, 16 * hd))
+    for rows in (dev(y), dev(bits(y)).view(torch.bfloat16)):
+        kv, q = Guarded(pool), Guarded(np.full(T * nq * hd, 0x7FA5, np.uint16))
+        metro.op_rope_append(rows, T, nq, nkv, hd, dev(rope), 30, ints(pos), ints(slot), q.inner, kv.inner, n_pages)
+        turned = bf16_bits_to_f64(q.read(np.uint16)).reshape(T, -1)
+        np.testing.assert_array_equal(np.isnan(turned).all(axis=1), (pos < 0) | (pos >= 30))
+        got, left, places = kv.read(np.uint16).reshape(pool.shape), pool.copy(), D.tile_places(hd)
+        for s in slot[(slot >= 0) & (slot < end)]:
+            for c in range(2):
+                at = places[c][s % 16]
+                assert not np.isin(got[s // 16, c][:, at], NAN_BITS[2:]).any()
+                left[s // 16, c][:, at] = got[s // 16, c][:, at]
+        np.testing.assert_array_equal(got, left)
+
+
+@pytest.mark.parametrize("hd,G,n", [(64, 1, 5), (128, 4, 1), (128, 4, 7), (64, 8, 9), (128, 2, 40)])
+def test_tree_touches_nothing_outside(metro, hd, G, n):
+    """Workspaces of just the queried size and of less, row ranges, contexts and pages outside theirs: the rows that an item
+    has are written, and no others."""
+    rng = np.random.default_rng([hd, G, n])
+    nkv, rows, max_keys = 2, 2 * n + 3, 1500
+    nq, pages = G * nkv, 20
+    pool = bits(rng.standard_normal((pages, 2, nkv, 16 * hd)))
+    q = bits(rng.standard_normal((rows, nq, hd)))
+    kv, qd = dev(pool), dev(q)
+    ldb = -(-max_keys // 16)
+    wild = rng.choice(np.array([INT_MIN, -1, 0, 5, pages - 1, pages, INT_MAX], np.int64), size=(2, ldb))
+    need = metro.op_attn_tree_workspace(nq, nkv, hd, 2, rows, n, max_keys)
+    state = rows * nq * (hd + 2) * 4
+    assert need > 2 * state
+    cases = [([1, 1 + n, 1 + 2 * n], [1500 - n, 33]), ([-5, n, INT_MAX], [INT_MAX, INT_MIN]), ([INT_MIN, 0, rows], [7, 1400]),
+             ([rows, INT_MAX, INT_MAX], [1, 1]), ([n, 2, 2], [-9, 40])]
+    for size in (need, need - 4, 2 * state, 2 * state - 4, 0):
+        for cu, ctx in cases:
+            ws, out = Guarded(np.full(max(size, 4), 0xA5, np.uint8)), Guarded(np.full(rows * nq * hd, 0x7FA5, np.uint16))
+            metro.op_attn_tree(qd, kv, pages, nq, nkv, hd, 2, ints(cu), rows, ints(ctx), n, max_keys, ints(wild), ldb, out.inner,
+                               workspace=ws.inner.view(torch.float32) if size else None)
+            ws.read(np.uint8)
+            got = out.read(np.uint16).reshape(rows, -1)
+            mine = np.zeros(rows, bool)
+            for i in range(2):
+                lo = min(max(cu[i], 0), rows)
+                mine[lo:max(lo, min(min(max(cu[i + 1], 0), rows), lo + n))] = True
+            np.testing.assert_array_equal((got != 0x7FA5).any(axis=1), mine)
+            np.testing.assert_array_equal((got != 0x7FA5).all(axis=1), mine)
+
+
+def test_move_touches_nothing_outside(metro):
+    rng = np.random.default_rng(51)
+    nkv, hd, n_pages, end = 3, 64, 4, 64
+    pool = rng.integers(0, 1 << 16, size=(2, n_pages, 2, nkv, 16 * hd), dtype=np.uint16)
+    src = np.array([end, end - 1, -1, 5, 6, INT_MIN, INT_MAX, 7, 8, 9, end + 15], np.int64)
+    dst = np.array([1, end, 2, 10, INT_MAX, 3, 4, INT_MIN, end + 1, 0, end + 31], np.int64)
+    kv = Guarded(pool)
+    metro.op_kv_move(kv.inner, 2, n_pages, nkv, hd, ints(src), ints(dst), ints([INT_MIN, 4, INT_MAX]), 2, len(src))
+    np.testing.assert_array_equal(kv.read(np.uint16).reshape(pool.shape), D.kv_move(pool, hd, src, dst, [0, 4, len(src)]))
+
+
+@pytest.mark.parametrize("rows,vocab", [(1, 1), (3, 777), (5, 16385), (2, 128256)])
+def test_sample_touches_nothing_outside(metro, rows, vocab):
+    rng = np.random.default_rng([rows, vocab])
+    x = logits(rng, rows, vocab)
+    ws = Guarded(np.full(metro.op_sample_workspace(rows, vocab), 0xA5, np.uint8))
+    u = rng.random(rows).astype(np.float32)
+    for top_k in (0, 30, INT_MAX):
+        out, prob = Guarded(np.full(rows, -9, np.int32)), Guarded(np.full(rows, -1, np.float32))
+        metro.op_sample(dev(x), rows, vocab, dev(u), out.inner, top_k=ints([top_k] * rows), prob=prob.inner, workspace=ws.inner)
+        ws.read(np.uint8)
+        tokens, probs = out.read(np.int32), prob.read(np.float32)
+        for r in range(rows):
+            t, p = D.sample(x[r], float(u[r]), top_k=top_k)
+            assert tokens[r] == t and abs(float(probs[r]) - p) <= 2.0 ** -24 * p + 2.0 ** -28
+
+
 # --- together ------------------------------------------------------------------------
 
 
