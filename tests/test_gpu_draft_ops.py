@@ -661,6 +661,29 @@ def test_sample_last_kept_token_of_light_tails(metro):
     sample_case(metro, x, u, top_p=[0.9] * 12)
 
 
+@pytest.mark.parametrize("vocab", [300, 5000, 20000])
+def test_sample_last_kept_token_of_odd_rows(metro, vocab):
+    """Ties, signed zeros, crowded logits, infinities, NaN and one token alone, with u from 1 on."""
+    rng = np.random.default_rng([vocab, 43])
+    nan, inf = np.nan, np.inf
+    some = lambda share, a, b: np.where(rng.random(vocab) < share, np.float32(a), b)
+    steps = (-np.arange(vocab) // 300 / 8).astype(np.float32)
+    rng.shuffle(steps)
+    x = np.stack([np.full(vocab, 1.5), some(0.5, 2.0, 1.0), some(0.5, 0.0, -0.0), steps, 8.0 + 1e-3 * rng.random(vocab),
+                  1e-30 * rng.standard_normal(vocab), some(0.1, 3.0, -1e4 * rng.random(vocab)),
+                  1e6 + 64 * rng.integers(0, 3, vocab), some(0.7, -inf, rng.standard_normal(vocab)),
+                  some(0.7, nan, rng.standard_normal(vocab)), some(0.01, inf, rng.standard_normal(vocab)),
+                  np.where(np.arange(vocab) == 7, 2.0, nan), np.full(vocab, -inf)]).astype(np.float32)
+    x[:8] = clear_border(x[:8], np.ones(8))
+    rows = len(x)
+    u = rng.choice([1.0, 3.0, inf], rows)
+    pick = lambda *v: rng.choice(v, rows)
+    for kw in (dict(), dict(top_k=pick(1, 2, 100, 290, 10 ** 9)), dict(top_p=pick(0.05, 0.31, 0.9)), dict(min_p=pick(0.01, 0.5, 1.0)),
+               dict(min_p=pick(0.01, 0.9), top_k=pick(0, 97, 280), top_p=pick(1.0, 0.55, 0.99)), dict(temperature=np.zeros(rows))):
+        tokens = sample_case(metro, x, u, **kw)
+        assert tokens[11] == 7 and tokens[12] == -1
+
+
 def test_sample_odd_settings(metro):
     rng = np.random.default_rng(2)
     x = logits(rng, 8, 3001)
