@@ -22,9 +22,9 @@ namespace metro {
 // rows at a time where the rows' slots are four such keys, whatever row they begin
 // at, and one by one elsewhere.
 //
-// Bound by memory: 8180 rows of 48 heads of 128 in fp32, with norms, 306 MB in 58 us
-// (5.3 TB/s; 70 in a row of calls), a wave a (row, head) with 2-byte stores 124; 336
-// drafts' rows in bf16 5.9 us, one row 2.8, which is a launch.
+// Bound by memory: 8180 rows of 48 heads of 128 in fp32, with norms, 306 MB in 71 us
+// (4.3 TB/s, a third of it writes), a wave a (row, head) with 2-byte stores 124; 336
+// drafts' rows in bf16 5.9 us, one row 2.9, which is a launch.
 // ---------------------------------------------------------------------------
 template <bool F32>
 __device__ __forceinline__ void load8(const AppendArgs& a, size_t at, float (&x)[8]) {
@@ -198,10 +198,13 @@ hipError_t launch_rope_append(const AppendArgs& a, hipStream_t s) {
 // of the V^T tile (a key's two values there) for all moves of a group: eight moves
 // at a time, it reads the chunk at every source before it writes the first
 // destination, and writes in the list's order, so no other thread can come between
-// and no barrier is needed.  Grid: (chunks of a layer's heads, layers, groups).  Bound by the lines
-// that it touches: a key's 256 bytes of K lie in 16 of them, those of V as 2-byte
-// values in the 1 KiB that its four keys share, so 107 moves in 32 layers of 8 heads
-// read and write about 6 times their 28 MB (22 us; one sequence's 3 moves 3.8).
+// and no barrier is needed.  Grid: (chunks of a layer's heads, layers, groups).  A key's
+// 256 bytes of K lie in 16 lines, those of V as 2-byte values in the 1 KiB that its
+// four keys share, so 107 moves in 32 layers of 8 heads fetch 65 MB and write 18 for 14
+// and 14.  Bound by latency rather than by those (16 us at a copy's rate): the compiler
+// waits for a move's slot, and so for the chunk before it, ahead of each load, and holds
+// the eight chunks in 204 registers, two waves a SIMD (26 us, waves waiting 83% of the
+// time; one sequence's 3 moves 3.6 us).
 // ---------------------------------------------------------------------------
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 

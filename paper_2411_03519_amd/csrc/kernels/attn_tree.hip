@@ -16,13 +16,19 @@
 // significant bits, which costs a third of the matrix instructions.
 //
 // What bounds it.  One token a sequence: K and V, streamed at 5.0 TB/s (123
-// contexts of 256 .. 4096 keys, 142 us; 25 of them 33 us).  Trees of 8 to 32 tokens
-// read the same and are held up besides by the scores' way through the vector ALU
-// (exponentials, the split into hi + lo), which overlaps the matrix cores' only
-// between waves: 123 trees 204 us, 25 of 9 to 17 tokens 43 us.  512 columns after
-// 20000 to 30000 keys: matrix cores busy 39% of the time, vector ALU about as much,
-// 190 to 220 us, 530 to 460 TFLOP/s of the products asked for and half as many again
-// for lo (a large library product reaches 1211 on this card).  Two and four tiles a
+// contexts of 256 .. 4096 keys, 142 us, and 25 of them 27, 33 where the caches hold none
+// of it; the model's decode kernel takes 139 and 29 on the same inputs).  Trees of 8 to
+// 32 tokens read the same and are held up besides by the scores' way through the vector
+// ALU (exponentials, the split into hi + lo), which overlaps the matrix cores' only
+// between waves, and by the waits that the ring's kernel notes: 123 trees 209 to 240 us,
+// 25 of 9 to 17 tokens 43 us.  512 columns after 20000 to 30000 keys: matrix cores busy
+// 40% of the time, the vector ALU issuing 65% (matrix instructions among them), 206 to
+// 238 us, 490 to 425 TFLOP/s of the products asked for and half as many again for lo (a
+// large library product reaches 1211 on this card).  A chain's tiles of columns go
+// through all pairs of its item, those behind the tile's last query too, where every
+// weight is 0: 512 queries 43 us, 4096 of them 1018, 16 items of 512 271, for which
+// the model's prefill kernel takes 19, 211 and 92; after a context of 4096 keys 512
+// queries 114 against 127.  Two and four tiles a
 // wave against LDS or registers, scores of the next pair formed beside this one's
 // weights, and tiles of up to 64 columns with the pairs shared by two halves of the
 // workgroup gave nothing over this.
@@ -425,8 +431,11 @@ __global__ __launch_bounds__(kTreeWaves * 64) __attribute__((amdgpu_waves_per_eu
 
 // ---------------------------------------------------------------------------
 // Many columns: eight waves of one tile each against the same pairs, whose pages
-// go through LDS in a ring of four stages by direct loads, three of them on their
-// way while one is used.  Two such workgroups fit a CU.
+// go through LDS in a ring of four stages by direct loads, issued three pairs ahead.
+// As compiled, each turn waits before its first products until at most two or three of
+// a wave's six loads under way are outstanding (the queries' loads count as pending
+// through the loop), so little more than the last pair issued is on its way while one is
+// used: waves wait 39 to 64% of the time.  Two such workgroups fit a CU.
 // ---------------------------------------------------------------------------
 constexpr int kTreeSharedWaves = 8, kTreeStages = 4;
 
@@ -636,7 +645,7 @@ __global__ __launch_bounds__(256) void attn_tree_combine_many_kernel(TreeArgs a,
 }
 
 // Up to 32 columns an item: the kernel through registers, one or two tiles a wave; more: the shared one.  A split has
-// to be worth its states (a column's is 528 bytes written and read again, a pair of pages 16 KiB): at least an eighth
+// to be worth its states (a column's is 520 bytes written and read again, a pair of pages 16 KiB): at least an eighth
 // of its columns in pairs, and four.  More splits are made while max_keys would leave fewer than `full` workgroups; the
 // items are often shorter than it, hence some times the 256 CUs, and where the items alone are more than fit the chip at
 // once, the longest of them must not outlast the others.  Measured (us; heads 32 over 8 of 128 but for the 64 tokens'):

@@ -27,13 +27,16 @@
 // row is read again for them.  A bin of many tokens is cut into finer ones by the
 // bits of its logits until few are left or all are the same.
 //
-// What bounds it: the first launch the vector ALU (fp64, 18 operations a logit; 325
-// rows of 128256 logits 71 us, 2.4 TB/s; a row in fewer, larger workgroups 78), one
-// row 9.7 us from end to end; the second the latency of its some 15 barriers and of
-// what every wave forms alike between them, 11 to 17 us a row whose bins are listed, up
-// to 35 where the row is read again or its bins are crowded (marked tokens fetched two
-// or four at a time, or the lists with the maxima, gave nothing).  One workgroup a row for
-// everything, with weights in fp64 exp(): 344 us for one row, 764 for 325.
+// What bounds it: the first launch the vector ALU, which issues 87% of the time (49
+// instructions a logit, 16 of them fp64; LDS is active 39%, a third of that in
+// conflicts; 325 rows of 128256 logits 71 to 76 us, 2.3 TB/s; a row in fewer, larger
+// workgroups 78), one row 9.7 us from end to end; the second the latency of its some 15
+// barriers and of what every wave forms alike between them, 11 to 17 us a row whose
+// bins are listed, up to 36 where the row is read again or its bins are crowded (marked
+// tokens fetched two or four at a time, or the lists with the maxima, gave nothing), and
+// its 90 KB of LDS and 127 registers, which leave a CU one workgroup: more than 256 rows
+// go in two rounds.  One workgroup a row for everything, with weights in fp64 exp():
+// 344 us for one row, 764 for 325.
 #include "common.h"
 #include "kernels.h"
 #include "kernels_draft.h"
